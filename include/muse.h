@@ -222,6 +222,82 @@ int exact_attn_bwd_static(const muse_params* p, const void* Q, const void* K, co
                           const void* O, const float* LSE, const void* dO,
                           void* dQ, void* dK, void* dV, void* stream);
 
+/* ---- Packed sequences -------------------------------------------------------------------------
+ * Exact causal attention (Eq. 1-2) over S sequences of different lengths whose tokens lie one after the other: sequence s has
+ * the rows cu_seqlens[s] .. cu_seqlens[s+1] - 1 of every tensor, and its tokens attend to their own sequence only.
+ *
+ * Row (t, h) of a tensor, D elements, starts at element t * token + h * head of it (muse_rows, in elements): [T, H, D] tensors,
+ * [H, T, D] ones and slices of a fused projection are all read and written where they are.  Rows start at 16-byte boundaries
+ * (pointers and strides).  Strides are not negative and a token stride is at most 2^22; an input may repeat rows (a stride of 0), the
+ * rows of an output must be distinct.  Outputs must not share elements with inputs or with each other.
+ *
+ * cu_seqlens [S+1] int32, device: not decreasing, within 0 .. T; equal neighbours are an empty sequence.  Rows in front of
+ * cu_seqlens[0] and from cu_seqlens[S] on belong to no sequence: what the outputs hold there is left as it was.  Values outside 0 .. T
+ * are taken as 0 or T; other broken offsets give meaningless results but no access outside the tensors.
+ * Any Hq / Hkv; D is 64 or 128.  A row that is not finite reaches the results of its own sequence only (there, by 0 * inf, also results of
+ * up to 255 rows of either side that do not attend to it). */
+typedef struct { int64_t token, head; } muse_rows;
+typedef struct {
+  int32_t S;            /* sequences */
+  int32_t Hq, Hkv, D;
+  int32_t T;            /* rows (tokens) of the tensors, at most 2^27 */
+  int32_t max_len;      /* a bound on the lengths if the caller has one, 0 if not: it chooses between kernels, results do not depend on it */
+  int32_t dtype;        /* MUSE_DTYPE_*: element type of Q, K, V, O, dO */
+  int32_t grad_dtype;   /* of dQ, dK, dV: MUSE_DTYPE_FP32 or the same as dtype */
+  uint32_t flags;       /* 0 */
+  float scale;          /* 0 -> 1/sqrt(D) */
+  muse_rows q, k, v, o, dout, dq, dk, dv;   /* the forward does not look at the last four */
+} muse_packed_params;
+
+/* Device scratch of the packed entry points: which = MUSE_WS_EXACT_FWD or MUSE_WS_EXACT_BWD. */
+int muse_packed_workspace_bytes(const muse_packed_params* p, int which, size_t* bytes);
+
+/* O = softmax attention of every row, LSE [Hq, T] fp32 its log normaliser.  ws may be NULL if 0 bytes are asked for. */
+int exact_attn_packed_fwd(const muse_packed_params* p, const void* Q, const void* K, const void* V, const int32_t* cu_seqlens,
+                          void* O, float* LSE, void* ws, size_t ws_bytes, void* stream);
+/* Its gradient; O and LSE are the forward's.  Every sum has one owner and a fixed order: repeated calls return identical bits. */
+int exact_attn_packed_bwd(const muse_packed_params* p, const void* Q, const void* K, const void* V, const int32_t* cu_seqlens,
+                          const void* O, const float* LSE, const void* dO, void* dQ, void* dK, void* dV,
+                          void* ws, size_t ws_bytes, void* stream);
+
+/* ---- A paged cache of 8-bit keys and values ------------------------------------------------------
+ * The cache has `pages` pages of `page` tokens.  Per page and key/value head it holds
+ *   k_cache [pages, Hkv, page, D], v_cache [pages, Hkv, D, page]  e4m3 (OCP) bytes: a value stands for itself times its scale
+ *   k_scale, v_scale [pages, Hkv]  fp32
+ * (values with the dims first, so that the matrix instructions' operand is read as it lies).  The token at position x of sequence s is in
+ * page table[s][x / page], at place x % page.  Positions are int32, offsets into the cache 64 bits.
+ *   table [S, table_cols] int32, device.  Entries that no position below the length needs are not looked at; an entry outside 0 .. pages - 1
+ *     is a page without tokens (nothing is stored there, and nothing attends to it), and so are positions from table_cols * page on.
+ *   kv_lens [S] int32, device: the length of every sequence, the new tokens of the call included; a negative one counts as 0.
+ *   cu_new [S+1] int32, device: rows cu_new[s] .. cu_new[s+1] - 1 of the tensors are sequence s's new tokens (as cu_seqlens above), at
+ *     positions kv_lens[s] - n .. kv_lens[s] - 1.  NULL: one new token per sequence, row s (T must be S).  */
+typedef struct {
+  int32_t S, Hq, Hkv, D;
+  int32_t T;            /* rows of the new tokens' tensors */
+  int32_t pages, page;  /* page: 16, 32, 64 or 128 tokens */
+  int32_t table_cols;
+  int32_t max_new;      /* a bound on the new tokens of a sequence, 0 if there is none: launches are sized by it, results do not depend on it */
+  int32_t dtype;        /* of Q, O and the new K, V */
+  uint32_t flags;       /* 0 */
+  float scale;          /* of the logits; 0 -> 1/sqrt(D) */
+  muse_rows q, k, v, o; /* exact_attn_cache_append looks at k, v only, exact_attn_cache_fwd at q, o only */
+} muse_cache_params;
+
+/* Stores new keys and values.  The scale of a page is the least power of two, 2^-100 at the least, by which the largest finite
+ * magnitude stored in it so far stays within 448; values are rounded to nearest, ties to even.  A new token that raises the scale
+ * has the page's earlier values rounded again.  A page is begun anew when the token at place 0 is stored: what it held does not count.
+ * Infinities and NaN are stored as NaN.  Places behind the last stored token keep their bytes.  A page that is stored to must stand once in
+ * the table (pages that several sequences share may only be read).  Repeated calls give identical bytes. */
+int exact_attn_cache_append(const muse_cache_params* p, const void* K, const void* V, const int32_t* cu_new, const int32_t* kv_lens,
+                            const int32_t* table, void* k_cache, void* v_cache, float* k_scale, float* v_scale, void* stream);
+
+/* Causal attention of the new tokens' queries to their sequences' cached tokens: the query of position x to the positions 0 .. x.
+ * A query without any key (a position below 0, or no page) gets O = 0 and LSE = -inf.  LSE [Hq, T] fp32 (may be NULL). */
+int muse_cache_workspace_bytes(const muse_cache_params* p, size_t* bytes);
+int exact_attn_cache_fwd(const muse_cache_params* p, const void* Q, const int32_t* cu_new, const int32_t* kv_lens, const int32_t* table,
+                         const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
+                         void* O, float* LSE, void* ws, size_t ws_bytes, void* stream);
+
 /* Diagnostics for benchmarks (not part of the method; process-wide, not thread-safe, allocates HIP
  * events): after muse_profile_enable(1) every kernel the library launches is bracketed by HIP events on
  * its stream; muse_profile_report synchronises those events and writes one line per kernel name,

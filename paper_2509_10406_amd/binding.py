@@ -25,7 +25,9 @@ FLAG_BALANCED_ASSIGN = 8
 FLAG_DIPOLE = 16
 WS_CLUSTER, WS_FWD, WS_BWD, WS_EXACT_FWD, WS_EXACT_BWD = range(5)
 SYMBOLS = ["muse_workspace_bytes", "muse_cluster", "muse_kmeans_stream", "muse_fwd", "muse_bwd", "exact_attn_fwd", "exact_attn_bwd",
-           "exact_attn_bwd_static", "muse_profile_enable", "muse_profile_report", "muse_probe_peaks", "muse_strerror"]
+           "exact_attn_bwd_static", "muse_packed_workspace_bytes", "exact_attn_packed_fwd", "exact_attn_packed_bwd",
+           "exact_attn_cache_append", "muse_cache_workspace_bytes", "exact_attn_cache_fwd", "muse_profile_enable",
+           "muse_profile_report", "muse_probe_peaks", "muse_strerror"]
 STATIC_SCRATCH_BYTES = 64 << 20
 
 
@@ -98,6 +100,13 @@ def load():
         lib.muse_strerror.argtypes = [C.c_int]
         for n in SYMBOLS[:-1]:
             getattr(lib, n).restype = C.c_int
+        ptr, size = C.c_void_p, C.c_size_t
+        lib.muse_packed_workspace_bytes.argtypes = [ptr, C.c_int, ptr]
+        lib.muse_cache_workspace_bytes.argtypes = [ptr, ptr]
+        lib.exact_attn_packed_fwd.argtypes = [ptr] * 8 + [size, ptr]
+        lib.exact_attn_packed_bwd.argtypes = [ptr] * 12 + [size, ptr]
+        lib.exact_attn_cache_append.argtypes = [ptr] * 11
+        lib.exact_attn_cache_fwd.argtypes = [ptr] * 12 + [size, ptr]
         _lib = lib
     return _lib
 
@@ -265,6 +274,217 @@ def exact_attn_bwd_static(p: Params, Q, K, V, O, LSE, dO, out):
     _check(load().exact_attn_bwd_static(C.byref(pc), _ptr(Q), _ptr(K), _ptr(V), _ptr(O), _ptr(LSE), _ptr(dO), _ptr(dQ),
                                         _ptr(dK), _ptr(dV), _stream()), "exact_attn_bwd_static")
     return dQ, dK, dV
+
+
+# ---- packed sequences and the paged 8-bit cache ------------------------------------------------------------------
+class _Rows(C.Structure):
+    _fields_ = [("token", C.c_int64), ("head", C.c_int64)]
+
+
+class _PackedParams(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("S", "Hq", "Hkv", "D", "T", "max_len", "dtype", "grad_dtype")] + \
+               [("flags", C.c_uint32), ("scale", C.c_float)] + [(n, _Rows) for n in ("q", "k", "v", "o", "dout", "dq", "dk", "dv")]
+
+
+class _CacheParams(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("S", "Hq", "Hkv", "D", "T", "pages", "page", "table_cols", "max_new", "dtype")] + \
+               [("flags", C.c_uint32), ("scale", C.c_float)] + [(n, _Rows) for n in ("q", "k", "v", "o")]
+
+
+@dataclass(frozen=True)
+class PackedParams:
+    """S sequences packed into T rows; max_len: a bound on their lengths (0: none is known)."""
+    S: int
+    Hq: int
+    Hkv: int
+    T: int
+    D: int
+    max_len: int = 0
+    dtype: int = BF16
+    grad_dtype: int = FP32
+    scale: float = 0.0
+
+    def __post_init__(self):
+        object.__setattr__(self, "_c", _PackedParams(self.S, self.Hq, self.Hkv, self.D, self.T, self.max_len, self.dtype,
+                                                     self.grad_dtype, 0, self.scale))
+
+    torch_dtype = Params.torch_dtype
+    torch_grad_dtype = Params.torch_grad_dtype
+
+
+@dataclass(frozen=True)
+class CacheParams:
+    """S sequences with T new tokens; a cache of `pages` pages of `page` tokens; max_new: a bound on a sequence's new tokens (0: none)."""
+    S: int
+    Hq: int
+    Hkv: int
+    T: int
+    D: int
+    pages: int
+    page: int
+    table_cols: int
+    max_new: int = 0
+    dtype: int = BF16
+    scale: float = 0.0
+
+    def __post_init__(self):
+        object.__setattr__(self, "_c", _CacheParams(self.S, self.Hq, self.Hkv, self.D, self.T, self.pages, self.page, self.table_cols,
+                                                    self.max_new, self.dtype, 0, self.scale))
+
+    torch_dtype = Params.torch_dtype
+
+
+@dataclass
+class KVCache:
+    """k [pages, Hkv, page, D] and v [pages, Hkv, D, page] of e4m3 bytes (uint8), k_scale and v_scale [pages, Hkv] fp32."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+
+
+def kv_cache(p: CacheParams, device="cuda") -> KVCache:
+    """An empty cache (its contents are those of a page without tokens: they do not count)."""
+    return KVCache(torch.zeros(p.pages, p.Hkv, p.page, p.D, dtype=torch.uint8, device=device),
+                   torch.zeros(p.pages, p.Hkv, p.D, p.page, dtype=torch.uint8, device=device),
+                   torch.ones(p.pages, p.Hkv, device=device), torch.ones(p.pages, p.Hkv, device=device))
+
+
+def _packed_rows(rows: _Rows, t, what, T, H, D, dtype, dev):
+    """The strides of a [T, H, D] tensor into `rows`; its address."""
+    if t.shape != (T, H, D) or t.dtype != dtype or t.device != dev:
+        raise MuseError(f"{what}: expected {dtype} [{T}, {H}, {D}] on {dev}, got {t.dtype} {list(t.shape)} on {t.device}")
+    st = t.stride()
+    if st[2] != 1:
+        raise MuseError(f"{what}: the elements of a row must be adjacent (strides {st})")
+    rows.token, rows.head = st[0], st[1]
+    return t.data_ptr()
+
+
+def _whole(t, what, shape, dtype, dev):
+    """The address of a contiguous tensor."""
+    if t.shape != shape or t.dtype != dtype or t.device != dev or not t.is_contiguous():
+        raise MuseError(f"{what}: expected contiguous {dtype} {list(shape)} on {dev}, got {t.dtype} {list(t.shape)} "
+                        f"(strides {t.stride()}) on {t.device}")
+    return t.data_ptr()
+
+
+def _packed_call(name, dev, pc, *args):
+    """Calls an entry point on the current stream of the tensors' device."""
+    if dev.index == torch.cuda.current_device():
+        rc = getattr(load(), name)(C.byref(pc), *args, torch.cuda.current_stream(dev).cuda_stream)
+    else:
+        with torch.cuda.device(dev):
+            rc = getattr(load(), name)(C.byref(pc), *args, torch.cuda.current_stream(dev).cuda_stream)
+    _check(rc, name)
+
+
+def _scratch(bytes_, ws, dev):
+    """(address, size) of the caller's workspace, or of one from torch's allocator: a call's own, so that calls on several streams
+    and captured graphs do not meet in it."""
+    if ws is None:
+        ws = torch.empty(bytes_, dtype=torch.uint8, device=dev) if bytes_ else None
+    elif ws.device != dev or not ws.is_contiguous():
+        raise MuseError(f"workspace: expected a contiguous tensor on {dev}")
+    return (ws, ws.data_ptr(), ws.numel() * ws.element_size()) if ws is not None else (None, 0, 0)
+
+
+def _on_gpu(t):
+    if not t.is_cuda:
+        raise MuseError("device-resident tensors only")
+    return t.device
+
+
+def muse_packed_workspace_bytes(p: PackedParams, which: int) -> int:
+    """Scratch of exact_attn_packed_fwd (WS_EXACT_FWD) or exact_attn_packed_bwd (WS_EXACT_BWD) for [T, H, D] tensors."""
+    got, pc = C.c_size_t(0), _PackedParams.from_buffer_copy(p._c)
+    for n in ("q", "o", "dout", "dq"):
+        getattr(pc, n).token, getattr(pc, n).head = p.Hq * p.D, p.D
+    for n in ("k", "v", "dk", "dv"):
+        getattr(pc, n).token, getattr(pc, n).head = p.Hkv * p.D, p.D
+    _check(load().muse_packed_workspace_bytes(C.byref(pc), which, C.byref(got)), "muse_packed_workspace_bytes")
+    return got.value
+
+
+def _packed_bytes(p: PackedParams, which: int) -> int:
+    """muse_packed_workspace_bytes, asked once per params."""
+    key = "_ws%d" % which
+    got = p.__dict__.get(key)
+    if got is None:
+        got = muse_packed_workspace_bytes(p, which)
+        object.__setattr__(p, key, got)
+    return got
+
+
+def exact_attn_packed_fwd(p: PackedParams, Q, K, V, cu_seqlens, ws=None, out=None):
+    """Exact causal attention of packed sequences.  Q [T, Hq, D], K and V [T, Hkv, D] in any strides whose rows are adjacent elements at
+    16-byte boundaries, cu_seqlens [S + 1] int32.  Returns (O [T, Hq, D], LSE [Hq, T]); out: tensors to write them into."""
+    dev = _on_gpu(Q)
+    O, LSE = out if out is not None else (torch.empty(p.T, p.Hq, p.D, dtype=p.torch_dtype, device=dev),
+                                          torch.empty(p.Hq, p.T, dtype=torch.float32, device=dev))
+    t, pc = p.torch_dtype, _PackedParams.from_buffer_copy(p._c)
+    ptrs = (_packed_rows(pc.q, Q, "Q", p.T, p.Hq, p.D, t, dev), _packed_rows(pc.k, K, "K", p.T, p.Hkv, p.D, t, dev),
+            _packed_rows(pc.v, V, "V", p.T, p.Hkv, p.D, t, dev), _whole(cu_seqlens, "cu_seqlens", (p.S + 1,), torch.int32, dev),
+            _packed_rows(pc.o, O, "O", p.T, p.Hq, p.D, t, dev), _whole(LSE, "LSE", (p.Hq, p.T), torch.float32, dev))
+    keep, at, size = _scratch(_packed_bytes(p, WS_EXACT_FWD), ws, dev)
+    _packed_call("exact_attn_packed_fwd", dev, pc, *ptrs, at, size)
+    return O, LSE
+
+
+def exact_attn_packed_bwd(p: PackedParams, Q, K, V, cu_seqlens, O, LSE, dO, ws=None, out=None):
+    """The gradient of exact_attn_packed_fwd.  Returns (dQ, dK, dV) of grad_dtype, shaped as Q, K, V."""
+    dev = _on_gpu(Q)
+    t, gt, pc = p.torch_dtype, p.torch_grad_dtype, _PackedParams.from_buffer_copy(p._c)
+    dQ, dK, dV = out if out is not None else (torch.empty(p.T, h, p.D, dtype=gt, device=dev) for h in (p.Hq, p.Hkv, p.Hkv))
+    ptrs = (_packed_rows(pc.q, Q, "Q", p.T, p.Hq, p.D, t, dev), _packed_rows(pc.k, K, "K", p.T, p.Hkv, p.D, t, dev),
+            _packed_rows(pc.v, V, "V", p.T, p.Hkv, p.D, t, dev), _whole(cu_seqlens, "cu_seqlens", (p.S + 1,), torch.int32, dev),
+            _packed_rows(pc.o, O, "O", p.T, p.Hq, p.D, t, dev), _whole(LSE, "LSE", (p.Hq, p.T), torch.float32, dev),
+            _packed_rows(pc.dout, dO, "dO", p.T, p.Hq, p.D, t, dev), _packed_rows(pc.dq, dQ, "dQ", p.T, p.Hq, p.D, gt, dev),
+            _packed_rows(pc.dk, dK, "dK", p.T, p.Hkv, p.D, gt, dev), _packed_rows(pc.dv, dV, "dV", p.T, p.Hkv, p.D, gt, dev))
+    keep, at, size = _scratch(_packed_bytes(p, WS_EXACT_BWD), ws, dev)
+    _packed_call("exact_attn_packed_bwd", dev, pc, *ptrs, at, size)
+    return dQ, dK, dV
+
+
+def _cache_ptrs(p: CacheParams, cu_new, kv_lens, table, cache: KVCache, dev):
+    byte, f32 = torch.uint8, torch.float32
+    return ((_whole(cu_new, "cu_new", (p.S + 1,), torch.int32, dev) if cu_new is not None else 0,
+             _whole(kv_lens, "kv_lens", (p.S,), torch.int32, dev), _whole(table, "table", (p.S, p.table_cols), torch.int32, dev)),
+            (_whole(cache.k, "cache.k", (p.pages, p.Hkv, p.page, p.D), byte, dev), _whole(cache.v, "cache.v", (p.pages, p.Hkv, p.D, p.page), byte, dev),
+             _whole(cache.k_scale, "cache.k_scale", (p.pages, p.Hkv), f32, dev), _whole(cache.v_scale, "cache.v_scale", (p.pages, p.Hkv), f32, dev)))
+
+
+def exact_attn_cache_append(p: CacheParams, K, V, cu_new, kv_lens, table, cache: KVCache):
+    """Stores the new tokens' K and V [T, Hkv, D] into the cache.  cu_new [S + 1] (None: one token per sequence), kv_lens [S] (the new
+    tokens included) and table [S, table_cols] are int32."""
+    dev = _on_gpu(K)
+    pc = _CacheParams.from_buffer_copy(p._c)
+    kp, vp = (_packed_rows(getattr(pc, n), x, n.upper(), p.T, p.Hkv, p.D, p.torch_dtype, dev) for n, x in (("k", K), ("v", V)))
+    index, held = _cache_ptrs(p, cu_new, kv_lens, table, cache, dev)
+    _packed_call("exact_attn_cache_append", dev, pc, kp, vp, *index, *held)
+
+
+def muse_cache_workspace_bytes(p: CacheParams) -> int:
+    got = C.c_size_t(0)
+    _check(load().muse_cache_workspace_bytes(C.byref(p._c), C.byref(got)), "muse_cache_workspace_bytes")
+    return got.value
+
+
+def exact_attn_cache_fwd(p: CacheParams, Q, cu_new, kv_lens, table, cache: KVCache, ws=None, out=None):
+    """Causal attention of the new tokens' queries Q [T, Hq, D] to their sequences' cached tokens.  Returns (O [T, Hq, D], LSE [Hq, T])."""
+    dev = _on_gpu(Q)
+    O, LSE = out if out is not None else (torch.empty(p.T, p.Hq, p.D, dtype=p.torch_dtype, device=dev),
+                                          torch.empty(p.Hq, p.T, dtype=torch.float32, device=dev))
+    t, pc = p.torch_dtype, _CacheParams.from_buffer_copy(p._c)
+    qp, op = (_packed_rows(r, x, n, p.T, p.Hq, p.D, t, dev) for r, x, n in ((pc.q, Q, "Q"), (pc.o, O, "O")))
+    index, held = _cache_ptrs(p, cu_new, kv_lens, table, cache, dev)
+    need = p.__dict__.get("_ws")
+    if need is None:
+        need = muse_cache_workspace_bytes(p)
+        object.__setattr__(p, "_ws", need)
+    keep, at, size = _scratch(need, ws, dev)
+    _packed_call("exact_attn_cache_fwd", dev, pc, qp, *index, *held, op, _whole(LSE, "LSE", (p.Hq, p.T), torch.float32, dev), at, size)
+    return O, LSE
 
 
 def muse_profile_enable(on: bool):
