@@ -52,7 +52,7 @@ int check_common(const P* p) {
   if (p->dtype != MUSE_DTYPE_FP32 && p->dtype != MUSE_DTYPE_BF16) return MUSE_ERR_INVALID_ARG;
   if (!(p->scale >= 0.f) || isinf(p->scale)) return MUSE_ERR_INVALID_ARG;
   if (p->D != 64 && p->D != 128) return MUSE_ERR_UNSUPPORTED;
-  if (p->T > kMaxRows || p->S > (1 << 20) || p->Hq > 4096) return MUSE_ERR_UNSUPPORTED;
+  if (p->T > kMaxRows || p->S > (1 << 20) || p->Hq > 4096 || p->Hkv > 4096) return MUSE_ERR_UNSUPPORTED;
   return MUSE_OK;
 }
 
@@ -78,7 +78,10 @@ int cache_dims(const muse_cache_params* p, CacheDims* d) {
   if (rc) return rc;
   if (p->pages < 1 || p->table_cols < 1 || p->max_new < 0) return MUSE_ERR_INVALID_ARG;
   if (p->page != 16 && p->page != 32 && p->page != 64 && p->page != 128) return MUSE_ERR_UNSUPPORTED;
-  if ((long long)p->table_cols * p->page > 0x7fffffffll) return MUSE_ERR_UNSUPPORTED;  // positions are int32
+  // positions, rows of a group and units of work are int32
+  if ((long long)p->table_cols * p->page > 0x7fffffffll || (long long)p->T * (p->Hq / p->Hkv) > (1 << 29) ||
+      (long long)p->S * (((long long)p->table_cols * p->page + 255) / 256 + 1) > 0x7fffffffll)
+    return MUSE_ERR_UNSUPPORTED;
   *d = CacheDims{p->S, p->Hq, p->Hkv, p->D, p->T, p->pages, p->page, p->table_cols, p->max_new > 0 && p->max_new < p->T ? p->max_new : p->T,
                  p->dtype, p->scale > 0.f ? p->scale : 1.0f / sqrtf((float)p->D), {}, {}, {}, {}};
   return MUSE_OK;

@@ -1,4 +1,4 @@
-// Exact attention over packed sequences and over the paged cache, one wave per row: online softmax over 64 keys at a time, a key
+// Exact attention over packed sequences, one wave per row: online softmax over 64 keys at a time, a key
 // per lane for the scores and D / 64 dims per lane for the sums.  Reads a key's row once per query, so it is bound by the caches.
 #include <type_traits>
 
@@ -116,57 +116,6 @@ __global__ void __launch_bounds__(64) k_packed_dkv_simple(PackedDims d, const T*
   }
 }
 
-__device__ __forceinline__ float e4m3_value(uint32_t b) {  // exact; S.1111.111 is NaN
-  const uint32_t e = (b >> 3) & 15, m = b & 7;
-  float v = e ? __uint_as_float(((e + 120) << 23) | (m << 20)) : (float)m * 0x1p-9f;
-  if ((b & 127) == 127) v = __builtin_nanf("");
-  return b & 128 ? -v : v;
-}
-
-template <typename T, int D>
-__global__ void __launch_bounds__(64) k_cache_fwd_simple(CacheDims d, const T* __restrict__ Q, const int32_t* __restrict__ cu, const int32_t* __restrict__ lens,
-                                                         const int32_t* __restrict__ table, const uint8_t* __restrict__ kc, const uint8_t* __restrict__ vc,
-                                                         const float* __restrict__ ks, const float* __restrict__ vs, T* __restrict__ O,
-                                                         float* __restrict__ LSE) {
-  __shared__ float q[D];
-  const int h = blockIdx.y, hk = h / (d.Hq / d.Hkv), lane = threadIdx.x;
-  const SeqTile st = seq_tile(cu, d.S, d.T, 1, blockIdx.x);
-  if (!st.ok) return;
-  const int n = st.beg + st.t, L = max(lens[st.s], 0);
-  const long long pos = (long long)L - (st.end - n), most = (long long)d.cols * d.page;
-  const int keys = (int)(pos + 1 < most ? pos + 1 : most);
-  row_to_lds<T, D>(Q + d.q.at(n, h), q);
-  __syncthreads();
-  float m = MUSE_NEG_INF, l = 0.f, o[D / 64] = {};
-  for (int k0 = 0; k0 < keys; k0 += 64) {
-    const int j = k0 + lane;
-    const int pid = j < keys ? table[(size_t)st.s * d.cols + j / d.page] : -1;
-    const bool live = pid >= 0 && pid < d.pages;
-    const size_t ph = (size_t)(live ? pid : 0) * d.Hkv + hk;
-    float s = MUSE_NEG_INF;
-    if (live) {
-      const uint8_t* row = kc + (ph * d.page + j % d.page) * D;
-      float a = 0.f;
-      for (int x = 0; x < D; ++x) a = fmaf(e4m3_value(row[x]), q[x], a);
-      s = a * ks[ph] * d.scale;
-    }
-    const float mn = fmaxf(m, wave_max(s)), ref = mn == MUSE_NEG_INF ? 0.f : mn, al = __expf(m - ref), p = __expf(s - ref);
-    m = mn;
-    l = l * al + wave_sum(p);
-    for (int x = 0; x < D / 64; ++x) o[x] *= al;
-    for (int i = 0; i < min(64, keys - k0); ++i) {
-      const int pi = __shfl(pid, i, 64);
-      const float w = __shfl(p, i, 64);
-      if (pi < 0 || pi >= d.pages) continue;
-      const size_t vh = (size_t)pi * d.Hkv + hk;
-      for (int x = 0; x < D / 64; ++x)
-        o[x] = fmaf(w * vs[vh], e4m3_value(vc[(vh * D + lane + 64 * x) * d.page + (k0 + i) % d.page]), o[x]);
-    }
-  }
-  for (int x = 0; x < D / 64; ++x) Elem<T>::st(O + d.o.at(n, h), lane + 64 * x, l > 0.f || l != l ? o[x] / l : 0.f);
-  if (LSE && lane == 0) LSE[(size_t)h * d.T + n] = m + __logf(l);
-}
-
 }  // namespace
 
 int muse_launch_packed_fwd(const PackedDims& d, const void* Q, const void* K, const void* V, const int32_t* cu, void* O, float* LSE, void* ws, hipStream_t st) {
@@ -201,21 +150,5 @@ int muse_launch_packed_bwd(const PackedDims& d, const void* Q, const void* K, co
   return MUSE_OK;
 }
 
-int muse_launch_cache_fwd(const CacheDims& d, const void* Q, const int32_t* cu, const int32_t* lens, const int32_t* table, const void* kc, const void* vc,
-                          const float* ks, const float* vs, void* O, float* LSE, void* ws, hipStream_t st) {
-  (void)ws;
-  const dim3 g((unsigned)packed_slots(d.T, d.S, 1), d.Hq);
-  MuseProf prof_("k_cache_fwd", st);
-  auto go = [&](auto* kernel, auto* t) {
-    using E = std::remove_pointer_t<decltype(t)>;
-    hipLaunchKernelGGL(kernel, g, dim3(64), 0, st, d, (const E*)Q, cu, lens, table, (const uint8_t*)kc, (const uint8_t*)vc, ks, vs, (E*)O, LSE);
-  };
-  if (d.dtype == MUSE_DTYPE_BF16) d.D == 64 ? go(k_cache_fwd_simple<bf16_t, 64>, (bf16_t*)0) : go(k_cache_fwd_simple<bf16_t, 128>, (bf16_t*)0);
-  else d.D == 64 ? go(k_cache_fwd_simple<float, 64>, (float*)0) : go(k_cache_fwd_simple<float, 128>, (float*)0);
-  MUSE_LAUNCH_CHECK();
-  return MUSE_OK;
-}
-
 size_t muse_packed_fwd_ws_bytes(const PackedDims&) { return 0; }
 size_t muse_packed_bwd_ws_bytes(const PackedDims& d) { return (size_t)d.Hq * d.T * 4; }
-size_t muse_cache_fwd_ws_bytes(const CacheDims&) { return 0; }
