@@ -234,7 +234,7 @@ int exact_attn_bwd_static(const muse_params* p, const void* Q, const void* K, co
  * cu_seqlens [S+1] int32, device: not decreasing, within 0 .. T; equal neighbours are an empty sequence.  Rows in front of
  * cu_seqlens[0] and from cu_seqlens[S] on belong to no sequence: what the outputs hold there is left as it was.  Values outside 0 .. T
  * are taken as 0 or T; other broken offsets give meaningless results but no access outside the tensors.
- * Any Hq / Hkv; D is 64 or 128.  A row that is not finite reaches the results of its own sequence only (there, by 0 * inf, also results of
+ * Any Hq / Hkv; D is 64 or 128; (T / 64 + S + 8) Hq up to 2^23.  A row that is not finite reaches the results of its own sequence only (there, by 0 * inf, also results of
  * up to 255 rows of either side that do not attend to it). */
 typedef struct { int64_t token, head; } muse_rows;
 typedef struct {

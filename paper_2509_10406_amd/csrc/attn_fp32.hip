@@ -15,6 +15,7 @@
 // Measured, 4 heads of 8k tokens, D = 64, blocks of 1024 (vector kernels with four lanes per query before): forward
 // 407 -> 63 us, dQ 494 -> 79 us, dK/dV 536 -> 105 us (about a third of the instruction rate; one wave per SIMD there).
 #include "fp32_sum.h"
+#include "packed.h"
 
 namespace {
 
@@ -46,15 +47,60 @@ __device__ __forceinline__ TileId tile_id(int tiles, bool last_first) {
   return r;
 }
 
+// What a workgroup works on.  Dense: [B, H, N, D] tensors in blocks of Bs rows, tiles of the whole sequence.  Packed: a sequence is the block,
+// tiles are the sequence's, and rows have strides of their own.
+struct DenseF32 {
+  static constexpr bool kPacked = false;
+  int N, Bs, Hq, Hkv, B;
+};
+struct PackedF32 {
+  static constexpr bool kPacked = true;
+  const int32_t* cu;
+  int S, T, Hq, Hkv, slots;
+  Rows r[8];  // Q, K, V, O, dO, dQ, dK, dV
+};
+struct F32Place {
+  int r0, beg, end, hq, hk;  // the tile's first row, its sequence's rows, the heads
+  size_t qh, kh;             // the head's first row: dense in the tensors, packed in LSE
+  bool ok;
+};
+__device__ __forceinline__ F32Place place_of(const DenseF32& l, bool keys) {
+  const TileId id = tile_id((l.N + 63) / 64, !keys);
+  const int G = l.Hq / l.Hkv, H = keys ? l.Hkv : l.Hq, h = id.row % H, b = id.row / H, hk = keys ? h : h / G;
+  return {id.tile * 64, 0, l.N, keys ? h * G : h, hk, ((size_t)b * l.Hq + (keys ? h * G : h)) * l.N, ((size_t)b * l.Hkv + hk) * l.N, true};
+}
+__device__ __forceinline__ F32Place place_of(const PackedF32& l, bool keys) {
+  const SeqTile s = packed_tile(l.cu, l.S, l.T, 64, keys ? l.Hkv : l.Hq, l.slots, !keys);
+  const int G = l.Hq / l.Hkv, hq = keys ? s.h * G : s.h;
+  return {s.beg + s.t * 64, s.beg, s.end, hq, hq / G, (size_t)hq * l.T, 0, s.ok};
+}
+// the first row of a row's block, and the first one behind it
+__device__ __forceinline__ int block_beg(const DenseF32& l, const F32Place&, int n) { return (n / l.Bs) * l.Bs; }
+__device__ __forceinline__ int block_beg(const PackedF32&, const F32Place& at, int) { return at.beg; }
+__device__ __forceinline__ int block_end(const DenseF32& l, const F32Place&, int n) { return (n / l.Bs + 1) * l.Bs; }
+__device__ __forceinline__ int block_end(const PackedF32&, const F32Place& at, int) { return at.end; }
+// head h of tensor i (its first row in dense tensors: `row`), and the distance of its rows
+template <int D>
+__device__ __forceinline__ size_t head_of(const DenseF32&, int, int, size_t row) { return row * D; }
+template <int D>
+__device__ __forceinline__ size_t head_of(const PackedF32& l, int i, int h, size_t) { return l.r[i].head * h; }
+template <int D>
+__device__ __forceinline__ size_t step_of(const DenseF32&, int) { return D; }
+template <int D>
+__device__ __forceinline__ size_t step_of(const PackedF32& l, int i) { return l.r[i].token; }
+// rows from one head to the next in LSE
+__device__ __forceinline__ size_t lse_rows(const DenseF32& l) { return l.N; }
+__device__ __forceinline__ size_t lse_rows(const PackedF32& l) { return l.T; }
+
 // rows r0 .. of X into registers (clamped addresses), and from there into LDS (rows past the end as zeros)
 template <int D>
-__device__ __forceinline__ void fetch_rows(const float* __restrict__ X, int r0, int N, float4 (&v)[4]) {
+__device__ __forceinline__ void fetch_rows(const float* __restrict__ X, int r0, int N, float4 (&v)[4], size_t step) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int c = threadIdx.x + 256 * i;
     int r = r0 + c / (D / 4);
     r = r < N ? r : N - 1;
-    v[i] = *reinterpret_cast<const float4*>(X + (size_t)r * D + 4 * (c % (D / 4)));
+    v[i] = *reinterpret_cast<const float4*>(X + r * step + 4 * (c % (D / 4)));
   }
 }
 template <int D>
@@ -71,10 +117,10 @@ __device__ __forceinline__ void commit_rows(float* lds, const float4 (&v)[4], in
 
 // the lane's column operand: dims 16u + 4h + t of row `row`, times mul; zeros for a row that is not there
 template <int D>
-__device__ __forceinline__ void load_col(const float* __restrict__ X, int row, bool live, int h, float mul, float (&y)[D / 4]) {
+__device__ __forceinline__ void load_col(const float* __restrict__ X, int row, bool live, int h, float mul, float (&y)[D / 4], size_t step) {
 #pragma unroll
   for (int u = 0; u < D / 16; ++u) {
-    const float4 x = live ? *reinterpret_cast<const float4*>(X + (size_t)row * D + 16 * u + 4 * h) : make_float4(0.f, 0.f, 0.f, 0.f);
+    const float4 x = live ? *reinterpret_cast<const float4*>(X + row * step + 16 * u + 4 * h) : make_float4(0.f, 0.f, 0.f, 0.f);
     y[4 * u] = mul * x.x; y[4 * u + 1] = mul * x.y; y[4 * u + 2] = mul * x.z; y[4 * u + 3] = mul * x.w;
   }
 }
@@ -155,40 +201,40 @@ __device__ __forceinline__ void store_col(const f32x4_t (&acc)[D / 16], float* _
     }
 }
 
-template <int D>
+template <int D, typename L>
 __global__ void __launch_bounds__(256, 2) k_attn_fwd_f32(const float* __restrict__ Q, const float* __restrict__ K,
                                                           const float* __restrict__ V, const float* __restrict__ ff,
-                                                          float* __restrict__ O, float* __restrict__ LSE, int N, int Bs,
-                                                          int Hq, int Hkv, int B, float scale) {
+                                                          float* __restrict__ O, float* __restrict__ LSE, L lay, float scale) {
   using A = F32Attn<D>;
   constexpr int R = A::kRows, LD = A::kLd;
   __shared__ __align__(16) float ks[R * LD];
   __shared__ __align__(16) float vs[R * LD];
-  const TileId id = tile_id((N + 63) / 64, true);
-  const int hq = id.row % Hq, b = id.row / Hq, hk = hq / (Hq / Hkv);
-  const size_t qh = ((size_t)b * Hq + hq) * N, kh = ((size_t)b * Hkv + hk) * N;
-  const int q0 = id.tile * 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const F32Place at = place_of(lay, false);
+  if (L::kPacked && !at.ok) return;
+  const size_t qh = at.qh, k_step = step_of<D>(lay, 1), v_step = step_of<D>(lay, 2);
+  const float *Kh = K + head_of<D>(lay, 1, at.hk, at.kh), *Vh = V + head_of<D>(lay, 2, at.hk, at.kh);
+  const int N = at.end, q0 = at.r0, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int c = threadIdx.x % 16, h = (threadIdx.x % 64) / 16;
   const int qa = q0 + 16 * w, qz = min(qa + 15, N - 1), n = qa + c;  // the wave's first and last query, the lane's
   const bool live = n < N;
-  const int beg_a = (qa / Bs) * Bs, beg_z = (qz / Bs) * Bs, beg = (n / Bs) * Bs;
+  const int beg_a = block_beg(lay, at, qa), beg_z = block_beg(lay, at, qz), beg = block_beg(lay, at, n);
   float q[D / 4];
-  load_col<D>(Q + qh * D, n, live, h, scale, q);
+  load_col<D>(Q + head_of<D>(lay, 0, at.hq, qh), n, live, h, scale, q, step_of<D>(lay, 0));
   f32x4_t acc[A::kAcc];
 #pragma unroll
   for (int i = 0; i < A::kAcc; ++i) acc[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   float m = MUSE_NEG_INF, l = 0.f;
-  const int kbeg = (q0 / Bs) * Bs, kend = min(q0 + 64, N);
+  const int kbeg = block_beg(lay, at, q0), kend = min(q0 + 64, N);
   float4 kr[4], vr[4];
-  fetch_rows<D>(K + kh * D, kbeg, N, kr);
-  fetch_rows<D>(V + kh * D, kbeg, N, vr);
+  fetch_rows<D>(Kh, kbeg, N, kr, k_step);
+  fetch_rows<D>(Vh, kbeg, N, vr, v_step);
   for (int k0 = kbeg; k0 < kend; k0 += R) {
     __syncthreads();
     commit_rows<D>(ks, kr, k0, N, 1.f);
     commit_rows<D>(vs, vr, k0, N, 1.f);
     __syncthreads();
-    fetch_rows<D>(K + kh * D, k0 + R, N, kr);
-    fetch_rows<D>(V + kh * D, k0 + R, N, vr);
+    fetch_rows<D>(Kh, k0 + R, N, kr, k_step);
+    fetch_rows<D>(Vh, k0 + R, N, vr, v_step);
     f32x4_t s[A::kSub];
     float mx = m;
 #pragma unroll
@@ -235,8 +281,8 @@ __global__ void __launch_bounds__(256, 2) k_attn_fwd_f32(const float* __restrict
   if (!live) return;
   float cf = 0.f;
   const float* f = ff + (qh + n) * D;
-  if (ff) {  // merge the far-field partial softmax state (max, sum, acc[D])
-    const float* fm = ff + (size_t)B * Hq * N * D + (qh + n) * 2;  // [acc | (max,sum)] planes
+  if constexpr (!L::kPacked) if (ff) {  // merge the far-field partial softmax state (max, sum, acc[D])
+    const float* fm = ff + (size_t)lay.B * lay.Hq * N * D + (qh + n) * 2;  // [acc | (max,sum)] planes
     const float mf = fm[0], lf = fm[1];
     if (lf > 0.f) {
       const float mn = fmaxf(m, mf), a = __expf(m - mn);
@@ -259,46 +305,46 @@ __global__ void __launch_bounds__(256, 2) k_attn_fwd_f32(const float* __restrict
       m = mn;
     }
   }
-  store_col<D>(acc, O + (qh + n) * D, h, 1.f / l);
+  store_col<D>(acc, O + head_of<D>(lay, 3, at.hq, qh) + n * step_of<D>(lay, 3), h, 1.f / l);
   if (h == 0) LSE[qh + n] = m + __logf(l);
 }
 
-template <int D>
+template <int D, typename L>
 __global__ void __launch_bounds__(256, 2) k_attn_bwd_dq_f32(const float* __restrict__ Q, const float* __restrict__ K,
                                                              const float* __restrict__ V, const float* __restrict__ dO,
                                                              const float* __restrict__ LSE, const float* __restrict__ delta,
-                                                             float* __restrict__ dQ, int N, int Bs, int Hq, int Hkv,
-                                                             float scale) {
+                                                             float* __restrict__ dQ, L lay, float scale) {
   using A = F32Attn<D>;
   constexpr int R = A::kRows, LD = A::kLd;
   __shared__ __align__(16) float ks[R * LD];
   __shared__ __align__(16) float vs[R * LD];
-  const TileId id = tile_id((N + 63) / 64, true);
-  const int hq = id.row % Hq, b = id.row / Hq, hk = hq / (Hq / Hkv);
-  const size_t qh = ((size_t)b * Hq + hq) * N, kh = ((size_t)b * Hkv + hk) * N;
-  const int q0 = id.tile * 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const F32Place at = place_of(lay, false);
+  if (L::kPacked && !at.ok) return;
+  const size_t qh = at.qh, k_step = step_of<D>(lay, 1), v_step = step_of<D>(lay, 2);
+  const float *Kh = K + head_of<D>(lay, 1, at.hk, at.kh), *Vh = V + head_of<D>(lay, 2, at.hk, at.kh);
+  const int N = at.end, q0 = at.r0, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int c = threadIdx.x % 16, h = (threadIdx.x % 64) / 16;
   const int qa = q0 + 16 * w, qz = min(qa + 15, N - 1), n = qa + c;
   const bool live = n < N;
-  const int beg_a = (qa / Bs) * Bs, beg_z = (qz / Bs) * Bs, beg = (n / Bs) * Bs;
+  const int beg_a = block_beg(lay, at, qa), beg_z = block_beg(lay, at, qz), beg = block_beg(lay, at, n);
   float q[D / 4], g[D / 4];
-  load_col<D>(Q + qh * D, n, live, h, scale, q);
-  load_col<D>(dO + qh * D, n, live, h, 1.f, g);
+  load_col<D>(Q + head_of<D>(lay, 0, at.hq, qh), n, live, h, scale, q, step_of<D>(lay, 0));
+  load_col<D>(dO + head_of<D>(lay, 4, at.hq, qh), n, live, h, 1.f, g, step_of<D>(lay, 4));
   const float lse = live ? LSE[qh + n] : 0.f, dl = live ? delta[qh + n] : 0.f;
   f32x4_t acc[A::kAcc];
 #pragma unroll
   for (int i = 0; i < A::kAcc; ++i) acc[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  const int kbeg = (q0 / Bs) * Bs, kend = min(q0 + 64, N);
+  const int kbeg = block_beg(lay, at, q0), kend = min(q0 + 64, N);
   float4 kr[4], vr[4];
-  fetch_rows<D>(K + kh * D, kbeg, N, kr);
-  fetch_rows<D>(V + kh * D, kbeg, N, vr);
+  fetch_rows<D>(Kh, kbeg, N, kr, k_step);
+  fetch_rows<D>(Vh, kbeg, N, vr, v_step);
   for (int k0 = kbeg; k0 < kend; k0 += R) {
     __syncthreads();
     commit_rows<D>(ks, kr, k0, N, 1.f);
     commit_rows<D>(vs, vr, k0, N, 1.f);
     __syncthreads();
-    fetch_rows<D>(K + kh * D, k0 + R, N, kr);
-    fetch_rows<D>(V + kh * D, k0 + R, N, vr);
+    fetch_rows<D>(Kh, k0 + R, N, kr, k_step);
+    fetch_rows<D>(Vh, k0 + R, N, vr, v_step);
 #pragma unroll
     for (int j = 0; j < A::kSub; ++j) {
       const int kj = k0 + 16 * j;
@@ -315,54 +361,55 @@ __global__ void __launch_bounds__(256, 2) k_attn_bwd_dq_f32(const float* __restr
       add_tile<D>(acc, ks + 16 * j * LD, ds, c, h, masked, [&](int r) { return kj + r >= beg && kj + r <= n; });
     }
   }
-  if (live) store_col<D>(acc, dQ + (qh + n) * D, h, scale);
+  if (live) store_col<D>(acc, dQ + head_of<D>(lay, 5, at.hq, qh) + n * step_of<D>(lay, 5), h, scale);
 }
 
 // loop over the query heads of the group and, inside, the queries n >= m of the key's block
-template <int D>
+template <int D, typename L>
 __global__ void __launch_bounds__(256, 2) k_attn_bwd_dkv_f32(const float* __restrict__ Q, const float* __restrict__ K,
                                                               const float* __restrict__ V, const float* __restrict__ dO,
                                                               const float* __restrict__ LSE, const float* __restrict__ delta,
-                                                              float* __restrict__ dK, float* __restrict__ dV, int N, int Bs,
-                                                              int Hq, int Hkv, float scale) {
+                                                              float* __restrict__ dK, float* __restrict__ dV, L lay, float scale) {
   using A = F32Attn<D>;
   constexpr int R = A::kRows, LD = A::kLd;
   __shared__ __align__(16) float qs[R * LD];
   __shared__ __align__(16) float gs[R * LD];
   __shared__ __align__(16) float ls[R];
   __shared__ __align__(16) float dls[R];
-  const TileId id = tile_id((N + 63) / 64, false);
-  const int hk = id.row % Hkv, b = id.row / Hkv, G = Hq / Hkv;
-  const size_t kh = ((size_t)b * Hkv + hk) * N;
-  const int k0 = id.tile * 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const F32Place at = place_of(lay, true);
+  if (L::kPacked && !at.ok) return;
+  const int N = at.end, G = lay.Hq / lay.Hkv;
+  const size_t kh = at.kh, q_step = step_of<D>(lay, 0), g_step = step_of<D>(lay, 4);
+  const int k0 = at.r0, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int c = threadIdx.x % 16, h = (threadIdx.x % 64) / 16;
   const int ka = k0 + 16 * w, kz = min(ka + 15, N - 1), m = ka + c;
   const bool live = m < N;
   // queries end with the block of the key; a tile may straddle blocks
-  const int end_a = (ka / Bs + 1) * Bs, end_z = min((kz / Bs + 1) * Bs, N), end = min((m / Bs + 1) * Bs, N);
-  const int qend = min((min(k0 + 63, N - 1) / Bs + 1) * Bs, N);
+  const int end_a = block_end(lay, at, ka), end_z = min(block_end(lay, at, kz), N), end = min(block_end(lay, at, m), N);
+  const int qend = min(block_end(lay, at, min(k0 + 63, N - 1)), N);
   float k[D / 4], v[D / 4];
-  load_col<D>(K + kh * D, m, live, h, 1.f, k);
-  load_col<D>(V + kh * D, m, live, h, 1.f, v);
+  load_col<D>(K + head_of<D>(lay, 1, at.hk, kh), m, live, h, 1.f, k, step_of<D>(lay, 1));
+  load_col<D>(V + head_of<D>(lay, 2, at.hk, kh), m, live, h, 1.f, v, step_of<D>(lay, 2));
   f32x4_t ak[A::kAcc], av[A::kAcc];
 #pragma unroll
   for (int i = 0; i < A::kAcc; ++i) ak[i] = av[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   for (int gh = 0; gh < G; ++gh) {
-    const size_t qh = ((size_t)b * Hq + (size_t)hk * G + gh) * N;
+    const size_t qh = at.qh + gh * lse_rows(lay);
+    const float *Qh = Q + head_of<D>(lay, 0, at.hq + gh, qh), *Gh = dO + head_of<D>(lay, 4, at.hq + gh, qh);
     float4 qr[4], gr[4];
     float lr = 0.f, dr = 0.f;
     const int lrow = threadIdx.x % R;
     if constexpr (D == 64) {  // the next rows are in flight while these are used; at D = 128 the registers are the operands'
-      fetch_rows<D>(Q + qh * D, k0, N, qr);
-      fetch_rows<D>(dO + qh * D, k0, N, gr);
+      fetch_rows<D>(Qh, k0, N, qr, q_step);
+      fetch_rows<D>(Gh, k0, N, gr, g_step);
     }
     lr = LSE[qh + min(k0 + lrow, N - 1)];
     dr = delta[qh + min(k0 + lrow, N - 1)];
     for (int q0 = k0; q0 < qend; q0 += R) {
       __syncthreads();
       if constexpr (D != 64) {
-        fetch_rows<D>(Q + qh * D, q0, N, qr);
-        fetch_rows<D>(dO + qh * D, q0, N, gr);
+        fetch_rows<D>(Qh, q0, N, qr, q_step);
+        fetch_rows<D>(Gh, q0, N, gr, g_step);
       }
       commit_rows<D>(qs, qr, q0, N, scale);
       commit_rows<D>(gs, gr, q0, N, 1.f);
@@ -372,8 +419,8 @@ __global__ void __launch_bounds__(256, 2) k_attn_bwd_dkv_f32(const float* __rest
       }
       __syncthreads();
       if constexpr (D == 64) {
-        fetch_rows<D>(Q + qh * D, q0 + R, N, qr);
-        fetch_rows<D>(dO + qh * D, q0 + R, N, gr);
+        fetch_rows<D>(Qh, q0 + R, N, qr, q_step);
+        fetch_rows<D>(Gh, q0 + R, N, gr, g_step);
       }
       lr = LSE[qh + min(q0 + R + lrow, N - 1)];
       dr = delta[qh + min(q0 + R + lrow, N - 1)];
@@ -401,8 +448,8 @@ __global__ void __launch_bounds__(256, 2) k_attn_bwd_dkv_f32(const float* __rest
     }
   }
   if (!live) return;
-  store_col<D>(ak, dK + (kh + m) * D, h, 1.f);
-  store_col<D>(av, dV + (kh + m) * D, h, 1.f);
+  store_col<D>(ak, dK + head_of<D>(lay, 6, at.hk, kh) + m * step_of<D>(lay, 6), h, 1.f);
+  store_col<D>(av, dV + head_of<D>(lay, 7, at.hk, kh) + m * step_of<D>(lay, 7), h, 1.f);
 }
 
 }  // namespace
@@ -410,11 +457,12 @@ __global__ void __launch_bounds__(256, 2) k_attn_bwd_dkv_f32(const float* __rest
 int muse_launch_attn_fwd_f32(const MuseDims& d, int Bs, const float* Q, const float* K, const float* V, const float* ff,
                              float* O, float* LSE, hipStream_t st) {
   const dim3 g((unsigned)(((d.N + 63) / 64) * d.Hq * d.B));
+  const DenseF32 lay{d.N, Bs, d.Hq, d.Hkv, d.B};
   MuseProf prof_("k_attn_fwd_f32", st);
   if (d.D == 64)
-    hipLaunchKernelGGL((k_attn_fwd_f32<64>), g, dim3(256), 0, st, Q, K, V, ff, O, LSE, d.N, Bs, d.Hq, d.Hkv, d.B, d.scale);
+    hipLaunchKernelGGL((k_attn_fwd_f32<64, DenseF32>), g, dim3(256), 0, st, Q, K, V, ff, O, LSE, lay, d.scale);
   else
-    hipLaunchKernelGGL((k_attn_fwd_f32<128>), g, dim3(256), 0, st, Q, K, V, ff, O, LSE, d.N, Bs, d.Hq, d.Hkv, d.B, d.scale);
+    hipLaunchKernelGGL((k_attn_fwd_f32<128, DenseF32>), g, dim3(256), 0, st, Q, K, V, ff, O, LSE, lay, d.scale);
   MUSE_LAUNCH_CHECK();
   return MUSE_OK;
 }
@@ -423,13 +471,42 @@ int muse_launch_attn_bwd_f32(const MuseDims& d, int Bs, const float* Q, const fl
                              const float* LSE, const float* delta, float* dQ, float* dK, float* dV, hipStream_t st) {
   const unsigned tiles = (unsigned)((d.N + 63) / 64) * d.B;
   const dim3 gq(tiles * d.Hq), gk(tiles * d.Hkv);
+  const DenseF32 lay{d.N, Bs, d.Hq, d.Hkv, d.B};
   if (d.D == 64) {
-    { MuseProf prof_("k_attn_bwd_dq_f32", st); hipLaunchKernelGGL((k_attn_bwd_dq_f32<64>), gq, dim3(256), 0, st, Q, K, V, dO, LSE, delta, dQ, d.N, Bs, d.Hq, d.Hkv, d.scale); }
-    { MuseProf prof_("k_attn_bwd_dkv_f32", st); hipLaunchKernelGGL((k_attn_bwd_dkv_f32<64>), gk, dim3(256), 0, st, Q, K, V, dO, LSE, delta, dK, dV, d.N, Bs, d.Hq, d.Hkv, d.scale); }
+    { MuseProf prof_("k_attn_bwd_dq_f32", st); hipLaunchKernelGGL((k_attn_bwd_dq_f32<64, DenseF32>), gq, dim3(256), 0, st, Q, K, V, dO, LSE, delta, dQ, lay, d.scale); }
+    { MuseProf prof_("k_attn_bwd_dkv_f32", st); hipLaunchKernelGGL((k_attn_bwd_dkv_f32<64, DenseF32>), gk, dim3(256), 0, st, Q, K, V, dO, LSE, delta, dK, dV, lay, d.scale); }
   } else {
-    { MuseProf prof_("k_attn_bwd_dq_f32", st); hipLaunchKernelGGL((k_attn_bwd_dq_f32<128>), gq, dim3(256), 0, st, Q, K, V, dO, LSE, delta, dQ, d.N, Bs, d.Hq, d.Hkv, d.scale); }
-    { MuseProf prof_("k_attn_bwd_dkv_f32", st); hipLaunchKernelGGL((k_attn_bwd_dkv_f32<128>), gk, dim3(256), 0, st, Q, K, V, dO, LSE, delta, dK, dV, d.N, Bs, d.Hq, d.Hkv, d.scale); }
+    { MuseProf prof_("k_attn_bwd_dq_f32", st); hipLaunchKernelGGL((k_attn_bwd_dq_f32<128, DenseF32>), gq, dim3(256), 0, st, Q, K, V, dO, LSE, delta, dQ, lay, d.scale); }
+    { MuseProf prof_("k_attn_bwd_dkv_f32", st); hipLaunchKernelGGL((k_attn_bwd_dkv_f32<128, DenseF32>), gk, dim3(256), 0, st, Q, K, V, dO, LSE, delta, dK, dV, lay, d.scale); }
   }
+  MUSE_LAUNCH_CHECK();
+  return MUSE_OK;
+}
+
+static PackedF32 packed_f32(const PackedDims& d, const int32_t* cu) {
+  return {cu, d.S, d.T, d.Hq, d.Hkv, (int)packed_slots(d.T, d.S, 64), {d.q, d.k, d.v, d.o, d.g, d.dq, d.dk, d.dv}};
+}
+
+int muse_launch_packed_fwd_f32(const PackedDims& d, const float* Q, const float* K, const float* V, const int32_t* cu, float* O, float* LSE, hipStream_t st) {
+  const PackedF32 lay = packed_f32(d, cu);
+  const dim3 g((unsigned)packed_grid(d.Hq, lay.slots));
+  MuseProf prof_("k_packed_fwd", st);
+  if (d.D == 64) hipLaunchKernelGGL((k_attn_fwd_f32<64, PackedF32>), g, dim3(256), 0, st, Q, K, V, nullptr, O, LSE, lay, d.scale);
+  else hipLaunchKernelGGL((k_attn_fwd_f32<128, PackedF32>), g, dim3(256), 0, st, Q, K, V, nullptr, O, LSE, lay, d.scale);
+  MUSE_LAUNCH_CHECK();
+  return MUSE_OK;
+}
+
+int muse_launch_packed_bwd_f32(const PackedDims& d, const float* Q, const float* K, const float* V, const int32_t* cu, const float* dO, const float* LSE,
+                               const float* delta, float* dQ, float* dK, float* dV, hipStream_t st) {
+  const PackedF32 lay = packed_f32(d, cu);
+  const dim3 gq((unsigned)packed_grid(d.Hq, lay.slots)), gk((unsigned)packed_grid(d.Hkv, lay.slots));
+  auto go = [&](auto* dq, auto* dkv) {
+    { MuseProf prof_("k_packed_dkv", st); hipLaunchKernelGGL(dkv, gk, dim3(256), 0, st, Q, K, V, dO, LSE, delta, dK, dV, lay, d.scale); }
+    { MuseProf prof_("k_packed_dq", st); hipLaunchKernelGGL(dq, gq, dim3(256), 0, st, Q, K, V, dO, LSE, delta, dQ, lay, d.scale); }
+  };
+  if (d.D == 64) go(k_attn_bwd_dq_f32<64, PackedF32>, k_attn_bwd_dkv_f32<64, PackedF32>);
+  else go(k_attn_bwd_dq_f32<128, PackedF32>, k_attn_bwd_dkv_f32<128, PackedF32>);
   MUSE_LAUNCH_CHECK();
   return MUSE_OK;
 }

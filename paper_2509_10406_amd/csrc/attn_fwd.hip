@@ -27,6 +27,7 @@
 #include "ff_common.h"
 #include "flash_tile.h"
 #include "lds_tile.h"
+#include "packed.h"
 
 namespace {
 
@@ -77,21 +78,59 @@ __device__ __forceinline__ void phase_end() {
 using lds_frag = __attribute__((address_space(3))) const bf16x8_t*;
 using lds_tr = __attribute__((address_space(3))) s16x4_t*;
 
-template <int D>
+// What a workgroup works on.  Dense: [B, H, N, D] tensors in blocks of Bs rows, with the far field's partial state ff.  Packed: a sequence
+// is the block, and rows have strides of their own.
+struct DenseRows {
+  static constexpr bool kPacked = false;
+  const float* ff;
+  int N, Bs, Hq, Hkv, nbatch, fold, tiles, chunk;
+};
+struct PackedRows {
+  static constexpr bool kPacked = true;
+  const int32_t* cu;
+  int S, T, Hq, Hkv, slots;
+  Rows r[4];  // Q, K, V, O
+};
+struct Place {
+  int beg, end, t, last;  // the block's rows; the tile is last - t (and, folded, t)
+  int hq, hk;
+  size_t qh, kh;          // the head's first row: dense in Q and K, packed in LSE
+};
+__device__ __forceinline__ FlashTile number_of(const DenseRows& l) {
+  return flash_tile_of((l.Bs + TR - 1) / TR, l.N / l.Bs, l.Hq, l.nbatch, l.tiles, l.chunk);
+}
+__device__ __forceinline__ SeqTile number_of(const PackedRows& l) { return packed_tile(l.cu, l.S, l.T, TR, l.Hq, l.slots); }
+__device__ __forceinline__ Place place_of(const DenseRows& l, const FlashTile& ft) {
+  const int hk = ft.h / (l.Hq / l.Hkv), beg = ft.blk * l.Bs;
+  return {beg, beg + l.Bs, ft.t, ft.tpg - 1, ft.h, hk, ((size_t)ft.b * l.Hq + ft.h) * l.N, ((size_t)ft.b * l.Hkv + hk) * l.N};
+}
+__device__ __forceinline__ Place place_of(const PackedRows& l, const SeqTile& s) {
+  return {s.beg, s.end, 0, s.t, s.h, s.h / (l.Hq / l.Hkv), (size_t)s.h * l.T, 0};
+}
+__device__ __forceinline__ int fold_of(const DenseRows& l) { return l.fold; }
+__device__ __forceinline__ int fold_of(const PackedRows&) { return 0; }
+__device__ __forceinline__ int64_t step_of(const DenseRows&, int) { return 0; }
+__device__ __forceinline__ int64_t step_of(const PackedRows& l, int i) { return l.r[i].token; }
+__device__ __forceinline__ size_t first_of(const DenseRows&, int, const Place&) { return 0; }
+__device__ __forceinline__ size_t first_of(const PackedRows& l, int i, const Place& at) { return l.r[i].head * (i == 1 || i == 2 ? at.hk : at.hq); }
+
+template <int D, typename L>
 __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) k_flash_fwd(
-    const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const bf16_t* __restrict__ V, const float* __restrict__ ff,
-    bf16_t* __restrict__ O, float* __restrict__ LSE, int N, int Bs, int Hq, int Hkv, int nbatch, int fold, int tiles, int chunk, float scale_log2e) {
+    const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const bf16_t* __restrict__ V, bf16_t* __restrict__ O, float* __restrict__ LSE, L lay,
+    float scale_log2e) {
   constexpr int KS = D / 16, DT = D / 32, CPR = D / 8, NCH = BN * CPR / 512, kTile = BN * D, NG = KS / 2, NF = 3;
   __shared__ __attribute__((aligned(256))) bf16_t ks[3][kTile];
   __shared__ __attribute__((aligned(256))) bf16_t vs[3][kTile];
-  const FlashTile ft = flash_tile_of((Bs + TR - 1) / TR, N / Bs, Hq, nbatch, tiles, chunk);
-  if (!ft.ok) return;
-  const int hq = ft.h, b = ft.b, hk = hq / (Hq / Hkv);
-  const size_t qh = ((size_t)b * Hq + hq) * N, kh = ((size_t)b * Hkv + hk) * N;
+  // The exit stands right behind the numbering: behind the rest of the place, the compiler spills twice as many registers at D = 128
+  // (blocks of 700, 32 heads of 4: 44.0 us for 40.8).
+  const auto num = number_of(lay);
+  if (!num.ok) return;
+  const Place at = place_of(lay, num);
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64, col = lane % 32, half = lane / 32;
   const bool late = wave >= 4;  // a phase behind
-  const int kbeg = ft.blk * Bs, bend = kbeg + Bs;  // the block; its last tile may have fewer than TR rows
-  const bf16_t *Kh = K + kh * D, *Vh = V + kh * D;
+  const int kbeg = at.beg, bend = at.end;
+  const int64_t q_step = L::kPacked ? step_of(lay, 0) : D, k_step = L::kPacked ? step_of(lay, 1) : D, v_step = L::kPacked ? step_of(lay, 2) : D;
+  const bf16_t *Kh = K + (L::kPacked ? first_of(lay, 1, at) : at.kh * D), *Vh = V + (L::kPacked ? first_of(lay, 2, at) : at.kh * D);
 
   // LDS addresses of this lane's operands (tile_row, tile_cols of lds_tile.h) in the first buffer: the other operands of a
   // step differ by a constant, or by an xor with a constant in the chunk bits.
@@ -100,14 +139,14 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
   // The chunk of a tile that this thread brings in: LDS takes them in order of the thread, so the swizzle is in the source.
   const int srow = tid / CPR, schunk = (tile_at<D>(srow, tid % CPR) - srow * D) / 8;  // the swizzle is its own inverse
 
-  for (int part = 0; part <= fold; ++part) {
-    const int t = part == 0 ? ft.tpg - 1 - ft.t : ft.t;  // long rows first
+  for (int part = 0; part <= fold_of(lay); ++part) {
+    const int t = part == 0 ? at.last - at.t : at.t;  // long rows first
     const int q0 = kbeg + t * TR;
     const int w0 = q0 + 32 * wave, nq = w0 + col, nqc = min(nq, bend - 1);
     const int kend = min(q0 + TR, bend), nt = (kend - kbeg + BN - 1) / BN;
     bf16x8_t qf[KS];
 #pragma unroll
-    for (int x = 0; x < KS; ++x) qf[x] = *reinterpret_cast<const bf16x8_t*>(Q + (qh + nqc) * D + 16 * x + 8 * half);
+    for (int x = 0; x < KS; ++x) qf[x] = *reinterpret_cast<const bf16x8_t*>(Q + (L::kPacked ? first_of(lay, 0, at) + nqc * q_step : (at.qh + nqc) * D) + 16 * x + 8 * half);
 
     // K(c) and V(c-1) into their buffers, straight from memory to LDS.  No branch: behind one, every LDS read in flight would
     // be waited for.  Rows past the block's end are its last row again, whose scores are masked or whose tile nobody reads.
@@ -115,13 +154,13 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
       using gptr = const __attribute__((address_space(1))) void*;
       using lptr = __attribute__((address_space(3))) void*;
       const int rk = min(kbeg + c * BN, bend - 1), rv = max(min(kbeg + c * BN - BN, bend - 1), kbeg);
-      const bf16_t *sk = Kh + (size_t)rk * D, *sv = Vh + (size_t)rv * D;
+      const bf16_t *sk = Kh + (size_t)rk * k_step, *sv = Vh + (size_t)rv * v_step;
       bf16_t *dk = ks[c % 3] + wave * 512, *dv = vs[(c + 2) % 3] + wave * 512;
 #pragma unroll
       for (int u = 0; u < NCH; ++u) {
         const int row = srow + BN / NCH * u;
-        __builtin_amdgcn_global_load_lds((gptr)(sk + (uint32_t)(min(row, bend - 1 - rk) * D + 8 * schunk)), (lptr)(dk + 4096 * u), 16, 0, 0);
-        __builtin_amdgcn_global_load_lds((gptr)(sv + (uint32_t)(min(row, bend - 1 - rv) * D + 8 * schunk)), (lptr)(dv + 4096 * u), 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((gptr)(sk + (uint32_t)(min(row, bend - 1 - rk) * (int)k_step + 8 * schunk)), (lptr)(dk + 4096 * u), 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((gptr)(sv + (uint32_t)(min(row, bend - 1 - rv) * (int)v_step + 8 * schunk)), (lptr)(dv + 4096 * u), 16, 0, 0);
       }
     };
     auto arrived = [&]() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); };
@@ -191,7 +230,12 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
           pf[h][G] = pack8(p, 2 * G, 2 * G + 1);
           const uint4 w = __builtin_bit_cast(uint4, pf[h][G]);
           any |= w.x | w.y | w.z | w.w;
-          psum = sum8(pf[h][G], psum);  // the normaliser sums the probabilities as the matrix cores see them
+          if constexpr (L::kPacked) {  // ... as they are: LSE is good to 32 bits, and a sum of half-step errors is less than one
+#pragma unroll
+            for (int e = 8 * G; e < 8 * G + 8; ++e) psum += p[e];
+          } else {
+            psum = sum8(pf[h][G], psum);  // the normaliser sums the probabilities as the matrix cores see them
+          }
           __builtin_amdgcn_sched_barrier(0);
           load(h, 2 * G, next);
           load(h, 2 * G + 1, next);
@@ -278,8 +322,8 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
     float cl = 1.f;                        // weight of the local part after the merge
     float cf = 0.f, lf = 0.f;
     const float* fa = nullptr;
-    if (ff) {
-      const float* fm = ff + (size_t)nbatch * Hq * N * D + (qh + nq) * 2;  // [acc | (max,sum)] planes
+    if constexpr (!L::kPacked) if (lay.ff) {
+      const float* fm = lay.ff + (size_t)lay.nbatch * lay.Hq * lay.N * D + (at.qh + nq) * 2;  // [acc | (max,sum)] planes
       const float mf = fm[0];
       lf = fm[1];
       if (lf > 0.f) {
@@ -287,7 +331,7 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
         cl = __expf(mnat - mx);
         cf = __expf(mf - mx);
         mnat = mx;
-        fa = ff + (qh + nq) * D;
+        fa = lay.ff + (at.qh + nq) * D;
       }
     }
     const float lt = l * cl + lf * cf;
@@ -306,9 +350,9 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
         }
 #pragma unroll
         for (int u = 0; u < 4; ++u) v[u] *= inv;
-        st4(O, (qh + nq) * D + d, v);
+        st4(O, (L::kPacked ? first_of(lay, 3, at) + nq * step_of(lay, 3) : (at.qh + nq) * D) + d, v);
       }
-    if (half == 0) LSE[qh + nq] = mnat + __logf(lt);
+    if (half == 0) LSE[at.qh + nq] = mnat + __logf(lt);
   }
 }
 
@@ -322,11 +366,24 @@ int muse_launch_attn_fwd_mfma(const MuseDims& d, int Bs, const void* Q, const vo
   const dim3 g = flash_grid_of(tiles, groups);
   MuseProf prof_("k_flash_fwd", st);
   auto go = [&](auto* kernel) {
-    hipLaunchKernelGGL(kernel, g, dim3(512), 0, st, (const bf16_t*)Q, (const bf16_t*)K, (const bf16_t*)V, ff, (bf16_t*)O, LSE, d.N,
-                       Bs, d.Hq, d.Hkv, d.B, fold, tiles, chunk, sl);
+    hipLaunchKernelGGL(kernel, g, dim3(512), 0, st, (const bf16_t*)Q, (const bf16_t*)K, (const bf16_t*)V, (bf16_t*)O, LSE,
+                       DenseRows{ff, d.N, Bs, d.Hq, d.Hkv, d.B, fold, tiles, chunk}, sl);
   };
-  if (d.D == 64) go(k_flash_fwd<64>);
-  else go(k_flash_fwd<128>);
+  if (d.D == 64) go(k_flash_fwd<64, DenseRows>);
+  else go(k_flash_fwd<128, DenseRows>);
+  MUSE_LAUNCH_CHECK();
+  return MUSE_OK;
+}
+
+int muse_launch_packed_fwd_mfma(const PackedDims& d, const void* Q, const void* K, const void* V, const int32_t* cu, void* O, float* LSE, hipStream_t st) {
+  const int slots = (int)packed_slots(d.T, d.S, TR);
+  MuseProf prof_("k_packed_fwd", st);
+  auto go = [&](auto* kernel) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)packed_grid(d.Hq, slots)), dim3(512), 0, st, (const bf16_t*)Q, (const bf16_t*)K, (const bf16_t*)V, (bf16_t*)O, LSE,
+                       PackedRows{cu, d.S, d.T, d.Hq, d.Hkv, slots, {d.q, d.k, d.v, d.o}}, d.scale * 1.4426950408889634f);
+  };
+  if (d.D == 64) go(k_flash_fwd<64, PackedRows>);
+  else go(k_flash_fwd<128, PackedRows>);
   MUSE_LAUNCH_CHECK();
   return MUSE_OK;
 }

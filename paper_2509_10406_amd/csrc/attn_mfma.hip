@@ -16,6 +16,7 @@
 #include "ff_common.h"
 #include "flash_tile.h"
 #include "lds_tile.h"
+#include "packed.h"
 
 namespace {
 
@@ -70,18 +71,18 @@ __device__ __forceinline__ void pair_unit(int c, int& pr, int& pc) {
 // A tile as it lies: chunk c = thread + 256 i is chunk c % (D / 8) of row c / (D / 8), so a load instruction takes whole rows,
 // and the tile in LDS (lds_tile.h) serves rows and transposed operands alike.
 template <int D>
-__device__ __forceinline__ uint4 fetch_row_chunk(const bf16_t* __restrict__ src, int r0, int N, int i) {
+__device__ __forceinline__ uint4 fetch_row_chunk(const bf16_t* __restrict__ src, int r0, int N, int i, size_t step) {
   const int c = threadIdx.x + 256 * i;
-  return *reinterpret_cast<const uint4*>(src + (size_t)min(r0 + c / (D / 8), N - 1) * D + c % (D / 8) * 8);
+  return *reinterpret_cast<const uint4*>(src + min(r0 + c / (D / 8), N - 1) * step + c % (D / 8) * 8);
 }
 template <int D>
-__device__ __forceinline__ void fetch_rows(const bf16_t* __restrict__ src, int r0, int N, TileRegs& r) {
+__device__ __forceinline__ void fetch_rows(const bf16_t* __restrict__ src, int r0, int N, TileRegs& r, size_t step = D) {
   static_assert(BN * (D / 8) / 256 == (D == 64 ? 2 : 4), "chunks per thread");
-  r.a = fetch_row_chunk<D>(src, r0, N, 0);
-  r.b = fetch_row_chunk<D>(src, r0, N, 1);
+  r.a = fetch_row_chunk<D>(src, r0, N, 0, step);
+  r.b = fetch_row_chunk<D>(src, r0, N, 1, step);
   if constexpr (D == 128) {
-    r.c = fetch_row_chunk<D>(src, r0, N, 2);
-    r.d = fetch_row_chunk<D>(src, r0, N, 3);
+    r.c = fetch_row_chunk<D>(src, r0, N, 2, step);
+    r.d = fetch_row_chunk<D>(src, r0, N, 3, step);
   }
 }
 template <int D>
@@ -105,49 +106,84 @@ __device__ __forceinline__ void commit_rows(const TileRegs& r, bf16_t* tile) {
 // both contractions; with a transposed copy (4-byte stores in row pairs, half of the LDS-active cycles in bank conflicts) and
 // two barriers per step it took, us before -> after, 989 -> 927 for exact attention of 32 heads of 8k, D = 128, 482 -> 460 at
 // 8 heads of 16k, 1821 -> 1779 at 16 heads of 64k in blocks of 8192, 3560 -> 3376 at 32; same bits.
-template <int D>
+struct DenseDq {  // [B, H, N, D] tensors in blocks of Bs rows
+  static constexpr bool kPacked = false;
+  int N, Bs, Hq, Hkv, nbatch;
+};
+struct PackedDq {  // packed sequences, rows with strides of their own
+  static constexpr bool kPacked = true;
+  const int32_t* cu;
+  int S, T, Hq, Hkv, slots;
+  Rows q, k, v, g, dq;
+};
+struct DqPlace {
+  int q0, N, beg, hq, hk;  // the tile's first query, the end of the rows that are its sequence's (packed: of the sequence), its block's first key
+  size_t qh, kh;           // the head's first row: dense in [B, H, N, ..], packed in LSE
+};
+__device__ __forceinline__ FlashTile number_of(const DenseDq& l) { return flash_tile(l.N, l.Bs, l.Hq, l.nbatch); }
+__device__ __forceinline__ SeqTile number_of(const PackedDq& l) { return packed_tile(l.cu, l.S, l.T, 128, l.Hq, l.slots); }
+__device__ __forceinline__ DqPlace place_of(const DenseDq& l, const FlashTile& ft) {
+  const int hk = ft.h / (l.Hq / l.Hkv), q0 = (ft.blk * ft.tpg + ft.tpg - 1 - ft.t) * 128;
+  return {q0, l.N, (q0 / l.Bs) * l.Bs, ft.h, hk, ((size_t)ft.b * l.Hq + ft.h) * l.N, ((size_t)ft.b * l.Hkv + hk) * l.N};
+}
+__device__ __forceinline__ DqPlace place_of(const PackedDq& l, const SeqTile& s) {
+  return {s.beg + s.t * 128, s.end, s.beg, s.h, s.h / (l.Hq / l.Hkv), (size_t)s.h * l.T, 0};
+}
+__device__ __forceinline__ size_t packed_at(const DenseDq&, int, int, int) { return 0; }
+__device__ __forceinline__ size_t packed_at(const PackedDq& l, int i, int h, int n) {
+  const Rows& r = i == 0 ? l.q : i == 1 ? l.k : i == 2 ? l.v : i == 3 ? l.g : l.dq;
+  return r.head * h + n * r.token;
+}
+__device__ __forceinline__ size_t packed_step(const DenseDq&, int) { return 0; }
+__device__ __forceinline__ size_t packed_step(const PackedDq& l, int i) { return i == 1 ? l.k.token : l.v.token; }
+__device__ __forceinline__ int block_of(const DenseDq& l, int n, int) { return (n / l.Bs) * l.Bs; }
+__device__ __forceinline__ int block_of(const PackedDq&, int, int beg) { return beg; }
+__device__ __forceinline__ bool straddles(const DenseDq& l) { return l.Bs % 128 != 0; }
+__device__ __forceinline__ bool straddles(const PackedDq&) { return false; }
+
+template <int D, typename OT, typename L>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2, D == 64 ? 3 : 2))) k_flash_bwd_dq(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K,
                                                        const bf16_t* __restrict__ V, const bf16_t* __restrict__ dO,
                                                        const float* __restrict__ LSE, const float* __restrict__ delta,
-                                                       float* __restrict__ dQ, int N, int Bs, int Hq, int Hkv,
-                                                       int nbatch, float scale, float scale_log2e) {
+                                                       OT* __restrict__ dQ, L lay, float scale, float scale_log2e) {
   constexpr int KS = D / 16, DT = D / 32;
   __shared__ __attribute__((aligned(256))) bf16_t ks[2][BN * D];
   __shared__ __attribute__((aligned(256))) bf16_t vs[2][BN * D];
-  const FlashTile ft = flash_tile(N, Bs, Hq, nbatch);
-  if (!ft.ok) return;
-  const int hq = ft.h, b = ft.b, hk = hq / (Hq / Hkv);
-  const size_t qh = ((size_t)b * Hq + hq) * N, kh = ((size_t)b * Hkv + hk) * N;
-  const int q0 = (ft.blk * ft.tpg + ft.tpg - 1 - ft.t) * 128;
+  const auto num = number_of(lay);
+  if (!num.ok) return;
+  const DqPlace at = place_of(lay, num);
+  const size_t qh = at.qh, kh = at.kh;
+  const int N = at.N, hq = at.hq, q0 = at.q0;
   const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, col = lane % 32, half = lane / 32;
   const int nq = q0 + 32 * wave + col;
   const int nqc = nq < N ? nq : N - 1;
-  const int myb = (nqc / Bs) * Bs;
+  const int myb = block_of(lay, nqc, at.beg);
 
   bf16x8_t qf[KS], gf[KS];
 #pragma unroll
   for (int s = 0; s < KS; ++s) {
-    qf[s] = *reinterpret_cast<const bf16x8_t*>(Q + (qh + nqc) * D + 16 * s + 8 * half);
-    gf[s] = *reinterpret_cast<const bf16x8_t*>(dO + (qh + nqc) * D + 16 * s + 8 * half);
+    qf[s] = *reinterpret_cast<const bf16x8_t*>(Q + (L::kPacked ? packed_at(lay, 0, hq, nqc) : (qh + nqc) * D) + 16 * s + 8 * half);
+    gf[s] = *reinterpret_cast<const bf16x8_t*>(dO + (L::kPacked ? packed_at(lay, 3, hq, nqc) : (qh + nqc) * D) + 16 * s + 8 * half);
   }
   const float lse2 = LSE[qh + nqc] * 1.4426950408889634f, dl = delta[qh + nqc];
-  const bool unaligned = (Bs % 128) != 0;
+  const bool unaligned = straddles(lay);
   f32x16_t dq[DT];
 #pragma unroll
   for (int t = 0; t < DT; ++t)
 #pragma unroll
     for (int e = 0; e < 16; ++e) dq[t][e] = 0.f;
 
-  const int kbeg = (q0 / Bs) * Bs, kend = min(q0 + 128, N);
-  const bf16_t *Kh = K + kh * D, *Vh = V + kh * D;
+  const int kbeg = at.beg, kend = min(q0 + 128, N);
+  const bf16_t *Kh = K + (L::kPacked ? packed_at(lay, 1, at.hk, 0) : kh * D), *Vh = V + (L::kPacked ? packed_at(lay, 2, at.hk, 0) : kh * D);
+  const size_t k_step = L::kPacked ? packed_step(lay, 1) : D, v_step = L::kPacked ? packed_step(lay, 2) : D;
   // two tiles in LDS, a third on its way in registers: a step has one barrier, the next tile is written in its middle
   TileRegs kreg, vreg;
-  fetch_rows<D>(Kh, kbeg, N, kreg);
-  fetch_rows<D>(Vh, kbeg, N, vreg);
+  fetch_rows<D>(Kh, kbeg, N, kreg, k_step);
+  fetch_rows<D>(Vh, kbeg, N, vreg, v_step);
   commit_rows<D>(kreg, ks[0]);
   commit_rows<D>(vreg, vs[0]);
-  fetch_rows<D>(Kh, kbeg + BN, N, kreg);
-  fetch_rows<D>(Vh, kbeg + BN, N, vreg);
+  fetch_rows<D>(Kh, kbeg + BN, N, kreg, k_step);
+  fetch_rows<D>(Vh, kbeg + BN, N, vreg, v_step);
   int buf = 0;
   for (int k0 = kbeg; k0 < kend; k0 += BN, buf ^= 1) {
     __syncthreads();
@@ -158,8 +194,8 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
       if (kt == 1) {  // past the end: some row of the sequence that nobody reads
         commit_rows<D>(kreg, ks[buf ^ 1]);
         commit_rows<D>(vreg, vs[buf ^ 1]);
-        fetch_rows<D>(Kh, k0 + 2 * BN, N, kreg);
-        fetch_rows<D>(Vh, k0 + 2 * BN, N, vreg);
+        fetch_rows<D>(Kh, k0 + 2 * BN, N, kreg, k_step);
+        fetch_rows<D>(Vh, k0 + 2 * BN, N, vreg, v_step);
       }
       if (!live) continue;
       f32x16_t s, dp;
@@ -201,8 +237,8 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       // every query row belongs to exactly one tile: the row is written, not added to
-      *reinterpret_cast<float4*>(dQ + (qh + nq) * D + 32 * t + 8 * g + 4 * half) =
-          make_float4(scale * dq[t][4 * g + 0], scale * dq[t][4 * g + 1], scale * dq[t][4 * g + 2], scale * dq[t][4 * g + 3]);
+      const float r4[4] = {scale * dq[t][4 * g + 0], scale * dq[t][4 * g + 1], scale * dq[t][4 * g + 2], scale * dq[t][4 * g + 3]};
+      st4(dQ, (L::kPacked ? packed_at(lay, 4, hq, nq) : (qh + nq) * D) + 32 * t + 8 * g + 4 * half, r4);
     }
 }
 
@@ -762,8 +798,9 @@ int muse_launch_attn_bwd_mfma(const MuseDims& d, int Bs, const void* Q, const vo
     if (int rc = muse_launch_attn_dq_wide(d, Bs, Q, K, V, dO, LSE, delta, dQacc, st)) return rc;
   } else {
     MuseProf prof_("k_flash_bwd_dq", st);
-    if (d.D == 64) hipLaunchKernelGGL(k_flash_bwd_dq<64>, gq, dim3(256), 0, st, q, k, v, g, LSE, delta, dQacc, d.N, Bs, d.Hq, d.Hkv, d.B, d.scale, sl);
-    else hipLaunchKernelGGL(k_flash_bwd_dq<128>, gq, dim3(256), 0, st, q, k, v, g, LSE, delta, dQacc, d.N, Bs, d.Hq, d.Hkv, d.B, d.scale, sl);
+    const DenseDq lay{d.N, Bs, d.Hq, d.Hkv, d.B};
+    if (d.D == 64) hipLaunchKernelGGL((k_flash_bwd_dq<64, float, DenseDq>), gq, dim3(256), 0, st, q, k, v, g, LSE, delta, dQacc, lay, d.scale, sl);
+    else hipLaunchKernelGGL((k_flash_bwd_dq<128, float, DenseDq>), gq, dim3(256), 0, st, q, k, v, g, LSE, delta, dQacc, lay, d.scale, sl);
   }
   if (to_lds && muse_attn_dkv_wide(d, Bs)) return muse_launch_attn_dkv_wide(d, Bs, Q, K, V, dO, LSE, delta, dKacc, dVacc, st);
   {
@@ -771,6 +808,20 @@ int muse_launch_attn_bwd_mfma(const MuseDims& d, int Bs, const void* Q, const vo
     if (d.D == 64) hipLaunchKernelGGL(k_flash_bwd_dkv_p<64>, gk, dim3(256), 0, st, q, k, v, g, LSE, delta, dKacc, dVacc, d.N, Bs, d.Hq, d.Hkv, d.B, d.scale, sl);
     else hipLaunchKernelGGL(k_flash_bwd_dkv128, gk, dim3(512), 0, st, q, k, v, g, LSE, delta, dKacc, dVacc, d.N, Bs, d.Hq, d.Hkv, d.B, d.scale, sl);
   }
+  MUSE_LAUNCH_CHECK();
+  return MUSE_OK;
+}
+
+// dQ of packed sequences whose lengths are short (attn_bwd.hip says where the line is)
+int muse_launch_packed_dq_narrow(const PackedDims& d, const void* Q, const void* K, const void* V, const int32_t* cu, const void* dO, const float* LSE,
+                                 const float* delta, void* dQ, hipStream_t st) {
+  const int slots = (int)packed_slots(d.T, d.S, 128);
+  auto go = [&](auto* kernel, auto* out) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)packed_grid(d.Hq, slots)), dim3(256), 0, st, (const bf16_t*)Q, (const bf16_t*)K, (const bf16_t*)V, (const bf16_t*)dO,
+                       LSE, delta, out, PackedDq{cu, d.S, d.T, d.Hq, d.Hkv, slots, d.q, d.k, d.v, d.g, d.dq}, d.scale, d.scale * 1.4426950408889634f);
+  };
+  if (d.grad_dtype == MUSE_DTYPE_BF16) d.D == 64 ? go(k_flash_bwd_dq<64, bf16_t, PackedDq>, (bf16_t*)dQ) : go(k_flash_bwd_dq<128, bf16_t, PackedDq>, (bf16_t*)dQ);
+  else d.D == 64 ? go(k_flash_bwd_dq<64, float, PackedDq>, (float*)dQ) : go(k_flash_bwd_dq<128, float, PackedDq>, (float*)dQ);
   MUSE_LAUNCH_CHECK();
   return MUSE_OK;
 }

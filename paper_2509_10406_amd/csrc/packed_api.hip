@@ -61,6 +61,7 @@ int packed_dims(const muse_packed_params* p, bool bwd, PackedDims* d) {
   if (rc) return rc;
   if (p->grad_dtype != MUSE_DTYPE_FP32 && p->grad_dtype != p->dtype) return MUSE_ERR_INVALID_ARG;
   if (p->max_len < 0) return MUSE_ERR_INVALID_ARG;
+  if (((long long)p->T / 64 + p->S + 8) * p->Hq > (1 << 23)) return MUSE_ERR_UNSUPPORTED;  // workgroups of a launch
   *d = PackedDims{p->S, p->Hq, p->Hkv, p->D, p->T, p->max_len > 0 && p->max_len < p->T ? p->max_len : p->T, p->dtype, p->grad_dtype,
                   p->scale > 0.f ? p->scale : 1.0f / sqrtf((float)p->D), {}, {}, {}, {}, {}, {}, {}, {}};
   if ((rc = make_rows(p->q, p->T, p->Hq, p->D, p->dtype, false, &d->q)) || (rc = make_rows(p->k, p->T, p->Hkv, p->D, p->dtype, false, &d->k)) ||

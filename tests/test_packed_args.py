@@ -55,14 +55,15 @@ COMMON = [(dict(S=0), INVALID), (dict(Hq=0), INVALID), (dict(Hkv=3), INVALID), (
           (dict(T=(1 << 27) + 1), UNSUPPORTED), (dict(Hq=8192), UNSUPPORTED)]
 
 
-@pytest.mark.parametrize("kw,rc", COMMON + [(dict(max_len=-1), INVALID), (dict(grad_dtype=2), INVALID), (dict(dtype=mb.FP32), INVALID)])
+@pytest.mark.parametrize("kw,rc", COMMON + [(dict(max_len=-1), INVALID), (dict(S=1 << 20), UNSUPPORTED), (dict(T=1 << 26), UNSUPPORTED), (dict(grad_dtype=2), INVALID), (dict(dtype=mb.FP32), INVALID)])
 def test_packed_params(kw, rc):
     assert fwd(packed(**kw)) == rc and bwd(packed(**kw)) == rc
 
 
 @pytest.mark.parametrize("kw,rc", COMMON + [(dict(pages=0), INVALID), (dict(table_cols=0), INVALID), (dict(max_new=-1), INVALID),
                                             (dict(page=48), UNSUPPORTED), (dict(page=8), UNSUPPORTED),
-                                            (dict(table_cols=1 << 27), UNSUPPORTED)])
+                                            (dict(table_cols=1 << 27), UNSUPPORTED), (dict(S=1 << 20, table_cols=1 << 24), UNSUPPORTED),
+                                            (dict(T=1 << 27, Hq=32), UNSUPPORTED)])
 def test_cache_params(kw, rc):
     assert append(cache(**kw)) == rc and attend(cache(**kw)) == rc
     got = C.c_size_t(0)
