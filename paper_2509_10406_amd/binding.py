@@ -371,12 +371,14 @@ def _whole(t, what, shape, dtype, dev):
 
 def _packed_call(name, dev, pc, *args):
     """Calls an entry point on the current stream of the tensors' device."""
-    if dev.index == torch.cuda.current_device():
-        rc = getattr(load(), name)(C.byref(pc), *args, torch.cuda.current_stream(dev).cuda_stream)
+    stream = torch._C._cuda_getCurrentRawStream(dev.index)  # without the object that torch.cuda.current_stream makes: a microsecond
+    if dev.index == torch._C._cuda_getDevice():
+        rc = getattr(load(), name)(C.byref(pc), *args, stream)
     else:
         with torch.cuda.device(dev):
-            rc = getattr(load(), name)(C.byref(pc), *args, torch.cuda.current_stream(dev).cuda_stream)
-    _check(rc, name)
+            rc = getattr(load(), name)(C.byref(pc), *args, stream)
+    if rc:
+        _check(rc, name)
 
 
 def _scratch(bytes_, ws, dev):

@@ -52,35 +52,27 @@ struct Chunk<bf16_t> {
   }
 };
 
+// page `pid` of one head: its places lo .. hi - 1 from the new rows
 template <typename T, int D, int PAGE>
-__global__ void __launch_bounds__(256) k_cache_append(CacheDims d, const T* __restrict__ K, const T* __restrict__ V, const int32_t* __restrict__ cu,
-                                                      const int32_t* __restrict__ lens, const int32_t* __restrict__ table, uint8_t* __restrict__ kc,
-                                                      uint8_t* __restrict__ vc, float* __restrict__ ks, float* __restrict__ vs) {
+__device__ __forceinline__ void append_page(const CacheDims& d, bool vals, int h, int beg, int L, int first, int col, int pid, const T* __restrict__ K,
+                                            const T* __restrict__ V, uint8_t* __restrict__ kc, uint8_t* __restrict__ vc, float* __restrict__ ks,
+                                            float* __restrict__ vs) {
   using C = Chunk<T>;
   constexpr int CPR = D / C::N, NP = (PAGE * CPR + 255) / 256, LD = PAGE + 4;  // chunks of a row, passes over a page
   __shared__ __attribute__((aligned(16))) uint8_t turn[D * LD];
   __shared__ float part[4];
-  const bool vals = blockIdx.z != 0;
-  const int h = blockIdx.y, tid = threadIdx.x;
-  const SeqTile st = seq_tile(cu, d.S, d.T, PAGE, blockIdx.x, 1);
-  const int n = st.end - st.beg;
-  if (n == 0 || st.t < 0) return;
-  const int L = max(lens[st.s], 0), first = L - n, p0 = max(first, 0);
-  const int col = p0 / PAGE + st.t;
-  if (col >= d.cols || (long long)col * PAGE >= L) return;
-  const int pid = table[(size_t)st.s * d.cols + col];
-  if (pid < 0 || pid >= d.pages) return;
-  const int x0 = col * PAGE, lo = max(p0, x0) - x0, hi = min(L - x0, PAGE);
-  const T* src = vals ? V + d.v.at(st.beg + x0 - first, h) : K + d.k.at(st.beg + x0 - first, h);  // of place 0; read from lo on
+  const int tid = threadIdx.x, x0 = col * PAGE, lo = max(max(first, 0), x0) - x0, hi = min(L - x0, PAGE);
   const int64_t step = vals ? d.v.token : d.k.token;
+  const T* src = (vals ? V + d.v.at(beg, h) : K + d.k.at(beg, h)) + (int64_t)(x0 - first) * step;  // of place 0; read from lo on
   uint4 v[NP];
-  float amax = 0.f;
 #pragma unroll
   for (int i = 0; i < NP; ++i) {
     const int c = tid + 256 * i, row = c / CPR;
     v[i] = make_uint4(0u, 0u, 0u, 0u);
     if (row >= lo && row < hi) v[i] = *reinterpret_cast<const uint4*>(src + row * step + (c % CPR) * C::N);
   }
+  if (pid < 0 || pid >= d.pages) return;  // asked for behind the rows: both are on their way together
+  float amax = 0.f;
 #pragma unroll
   for (int i = 0; i < NP; ++i)
 #pragma unroll
@@ -146,15 +138,47 @@ __global__ void __launch_bounds__(256) k_cache_append(CacheDims d, const T* __re
   }
 }
 
+// `every` > 0: number x is page x % every of sequence x / every's new tokens, and the ones `every` further on; else seq_tile's numbers.
+template <typename T, int D, int PAGE>
+__global__ void __launch_bounds__(256) k_cache_append(CacheDims d, int every, const T* __restrict__ K, const T* __restrict__ V, const int32_t* __restrict__ cu,
+                                                      const int32_t* __restrict__ lens, const int32_t* __restrict__ table, uint8_t* __restrict__ kc,
+                                                      uint8_t* __restrict__ vc, float* __restrict__ ks, float* __restrict__ vs) {
+  const bool vals = blockIdx.z != 0;
+  const int h = blockIdx.y;
+  SeqTile st;
+  if (every > 0) {
+    st.s = blockIdx.x / every;
+    st.t = blockIdx.x % every;
+    st.beg = seq_row(cu, st.s, d.T);
+    st.end = max(seq_row(cu, st.s + 1, d.T), st.beg);
+  } else {
+    st = seq_tile(cu, d.S, d.T, PAGE, blockIdx.x, 1);
+  }
+  const int n = st.end - st.beg;
+  if (n == 0 || st.t < 0) return;
+  const int L = max(lens[st.s], 0), first = L - n, p0 = max(first, 0);
+  for (int t = st.t;; t += every) {
+    const int col = p0 / PAGE + t;
+    if (col >= d.cols || (long long)col * PAGE >= L) return;
+    append_page<T, D, PAGE>(d, vals, h, st.beg, L, first, col, table[(size_t)st.s * d.cols + col], K, V, kc, vc, ks, vs);
+    if (every <= 0) return;
+    __syncthreads();
+  }
+}
+
 }  // namespace
 
 int muse_launch_cache_append(const CacheDims& d, const void* K, const void* V, const int32_t* cu, const int32_t* lens, const int32_t* table,
                              void* kc, void* vc, float* ks, float* vs, hipStream_t st) {
-  const dim3 g((unsigned)(packed_slots(d.T, d.S, d.page) + d.S), d.Hkv, 2);
+  // Pages that new tokens may touch: all together by their rows, or sequence by sequence by the bound on them, whichever is fewer
+  // (the second needs no search: 128 single tokens TBD).
+  const long long all = packed_slots(d.T, d.S, d.page) + d.S, each = (d.max_new + d.page - 2) / d.page + 1;
+  const int every = each * d.S <= all ? (int)each : 0;
+  const dim3 g((unsigned)(every ? each * d.S : all), d.Hkv, 2);
   MuseProf prof_("k_cache_append", st);
   auto go = [&](auto* kernel, auto* t) {
     using E = std::remove_pointer_t<decltype(t)>;
-    hipLaunchKernelGGL(kernel, g, dim3(256), 0, st, d, (const E*)K, (const E*)V, cu, lens, table, (uint8_t*)kc, (uint8_t*)vc, ks, vs);
+    hipLaunchKernelGGL(kernel, g, dim3(256), 0, st, d, every, (const E*)K, (const E*)V, cu, lens, table, (uint8_t*)kc, (uint8_t*)vc, ks, vs);
   };
 #define PAGES(E, DD)                                                 \
   switch (d.page) {                                                  \

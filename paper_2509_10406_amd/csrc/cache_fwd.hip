@@ -24,6 +24,7 @@
 namespace {
 
 constexpr int UNIT = 256;
+constexpr int JOIN = 8;  // rows of a workgroup of k_cache_join
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kLazy = 8.f;  // the softmax reference follows the maximum in steps of more than 2^8
 
@@ -66,9 +67,10 @@ struct Found {
 struct FindLds {
   int sum[4], most[4], before, s;
 };
-// The first unit of workgroup w's share.  Where there are fewer units than workgroups, the first of these have one each: a share in
-// the middle of a sequence is never empty.
+// The first unit of workgroup w's share, and whose share a unit is in.  Where there are fewer units than workgroups, the first of these
+// have one each: a share in the middle of a sequence is never empty.
 __device__ __forceinline__ int share(int total, int w, int W) { return total <= W ? min(w, total) : (int)((long long)total * w / W); }
+__device__ __forceinline__ int owner(int total, int unit, int W) { return total <= W ? unit : (int)((((long long)unit + 1) * W - 1) / total); }
 __device__ __forceinline__ Found find_unit(const CacheDims& d, const CacheWork& w, const int32_t* cu, const int32_t* lens, int r, int tile_last, FindLds& lds, int wg) {
   const int tid = threadIdx.x, lane = tid % 64, per = (d.S + 255) / 256, s0 = tid * per, s1 = min(s0 + per, d.S);
   int mine = 0, most = 0;
@@ -377,47 +379,70 @@ __global__ void __launch_bounds__(256, RT > 1 ? 1 : D == 64 && sizeof(T) == 2 ? 
 }
 
 // Joins the parts of the sequences that several workgroups share.  Workgroup x looks at the border between the shares x and x + 1: the first
-// border inside a sequence has that sequence.  A wave per row, the parts one after the other.
+// border inside a sequence has that sequence.  Bound by the latency of its reads, so a row's parts are asked for eight at a time and,
+// where there are many, by the four waves together (a quarter of them each, joined in order through LDS); few parts: a wave per row.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) k_cache_join(CacheDims d, CacheWork wk, const int32_t* __restrict__ cu, const int32_t* __restrict__ lens,
                                                     T* __restrict__ O, float* __restrict__ LSE) {
-  constexpr int DL = D / 64;
+  constexpr int DL = D / 64, FEW = 8;
   __shared__ FindLds find;
-  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64, w = blockIdx.x + 1, hk = blockIdx.y, r = blockIdx.z;
+  __shared__ float part[4][D + 1];
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64, w = blockIdx.x + 1, hk = blockIdx.y / (wk.rows / JOIN),
+            first = blockIdx.y % (wk.rows / JOIN) * JOIN, r = blockIdx.z;
   const int tile_last = last_token(wk, r);
   const Found f = find_unit(d, wk, cu, lens, r, tile_last, find, w);
   const int a = share(f.total, w, wk.W);
   if (a >= f.total || share(f.total, w - 1, wk.W) > f.before || a <= f.before) return;
   const Seg sg = seg_of(d, wk, cu, lens, f.s, r, tile_last);
-  const int end = f.before + sg.units;
-  int n = 1;  // parts: the workgroups w - 1, w, .. that begin in front of the sequence's end
-  while (w - 1 + n < wk.W && share(f.total, w - 1 + n, wk.W) < end) ++n;
+  const int n = owner(f.total, f.before + sg.units - 1, wk.W) - (w - 1) + 1;  // parts: of the workgroups w - 1, w, ..
   const size_t base = ((size_t)r * d.Hkv + hk) * 2 * wk.W;
   auto slot = [&](int i) { return (base + (i == 0 ? 2 * (w - 1) + 1 : 2 * (w - 1 + i))) * wk.rows; };
-  for (int q = wave; q < wk.rows; q += 4) {
-    const int y = r * wk.rows + q;
-    if (y >= sg.n * wk.G) break;
+  const bool together = n > FEW;
+  const int rows = min(first + JOIN, sg.n * wk.G - r * wk.rows);
+  for (int q = first + (together ? 0 : wave); q < rows; q += together ? 1 : 4) {
+    const int i0 = together ? n * wave / 4 : 0, i1 = together ? n * (wave + 1) / 4 : n;
     float M = MUSE_NEG_INF;
     for (int i = lane; i < n; i += 64) M = fmaxf(M, wk.pm[(slot(i) + q) * 2]);
     M = wave_max(M);
     float l = 0.f, v[DL] = {};
-    for (int i0 = 0; i0 < n; i0 += 64) {
+    for (int j0 = i0; j0 < i1; j0 += 64) {
       float fw = 0.f;
-      if (i0 + lane < n) {
-        const float2 p = *reinterpret_cast<const float2*>(wk.pm + (slot(i0 + lane) + q) * 2);
+      if (j0 + lane < i1) {
+        const float2 p = *reinterpret_cast<const float2*>(wk.pm + (slot(j0 + lane) + q) * 2);
         fw = M == MUSE_NEG_INF ? 0.f : exp2_(p.x - M);
         l += fw * p.y;
       }
-      for (int i = 0; i < min(64, n - i0); ++i) {
-        const float fi = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, fw), i));
-        const float* p = wk.po + (slot(i0 + i) + q) * D + lane * DL;
+      const int m = min(64, i1 - j0);
+      for (int k = 0; k < m; k += 8) {
+        float x[8][DL];
 #pragma unroll
-        for (int j = 0; j < DL; ++j) v[j] = fmaf(fi, p[j], v[j]);
+        for (int u = 0; u < 8; ++u) {
+          const float* p = wk.po + (slot(min(j0 + k + u, i1 - 1)) + q) * D + lane * DL;
+#pragma unroll
+          for (int j = 0; j < DL; ++j) x[u][j] = p[j];
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          const float fu = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, fw), k + u));
+#pragma unroll
+          for (int j = 0; j < DL; ++j) v[j] = k + u < m ? fmaf(fu, x[u][j], v[j]) : v[j];
+        }
       }
     }
     l = wave_sum(l);
+    if (together) {
+      __syncthreads();  // the row before has been read
+#pragma unroll
+      for (int j = 0; j < DL; ++j) part[wave][lane * DL + j] = v[j];
+      if (lane == 0) part[wave][D] = l;
+      __syncthreads();
+      if (wave != 0) continue;
+      l = (part[0][D] + part[1][D]) + (part[2][D] + part[3][D]);
+#pragma unroll
+      for (int j = 0; j < DL; ++j) v[j] = (part[0][lane * DL + j] + part[1][lane * DL + j]) + (part[2][lane * DL + j] + part[3][lane * DL + j]);
+    }
+    const int y = r * wk.rows + q, i = y / wk.G, h = hk * wk.G + y - i * wk.G;
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    const int i = y / wk.G, h = hk * wk.G + y - i * wk.G;
     T* to = O + d.o.at(sg.beg + i, h) + lane * DL;
 #pragma unroll
     for (int j = 0; j < DL; ++j) Elem<T>::st(to, j, v[j] * inv);
@@ -472,7 +497,7 @@ int muse_launch_cache_fwd(const CacheDims& d, const void* Q, const int32_t* cu, 
     }
     if (p.w.W > 1) {
       MuseProf prof_("k_cache_join", st);
-      hipLaunchKernelGGL(join, dim3(p.w.W - 1, d.Hkv, p.w.R), dim3(256), 0, st, d, p.w, cu, lens, (E*)O, LSE);
+      hipLaunchKernelGGL(join, dim3(p.w.W - 1, d.Hkv * (p.w.rows / JOIN), p.w.R), dim3(256), 0, st, d, p.w, cu, lens, (E*)O, LSE);
     }
   };
   if (d.dtype == MUSE_DTYPE_BF16) {

@@ -4,6 +4,7 @@
 #include "attn_bwd_wide.h"
 
 int muse_launch_packed_fwd_mfma(const PackedDims& d, const void* Q, const void* K, const void* V, const int32_t* cu, void* O, float* LSE, hipStream_t st);
+int muse_launch_packed_fwd_cols(const PackedDims& d, const void* Q, const void* K, const void* V, const int32_t* cu, void* O, float* LSE, hipStream_t st);
 int muse_launch_packed_fwd_f32(const PackedDims& d, const float* Q, const float* K, const float* V, const int32_t* cu, float* O, float* LSE, hipStream_t st);
 int muse_launch_packed_bwd_f32(const PackedDims& d, const float* Q, const float* K, const float* V, const int32_t* cu, const float* dO, const float* LSE,
                                const float* delta, float* dQ, float* dK, float* dV, hipStream_t st);
@@ -75,12 +76,21 @@ __global__ void __launch_bounds__(256) k_packed_delta(PackedDims d, int slots, c
 
 }  // namespace
 
+// Which kernels a call takes, by the bound on its lengths (the caller's, or all tokens).  us, tiles of 128 / of 256 rows, about 16k tokens:
+//   forward  D = 64: 40 sequences of 400 49 / 64 with 16 heads, 70 / 115 with 32 of 8; 16 of 1024 74 / 82 and 127 / 140; 8 of 2048 126 / 119
+//            and 209 / 198; 16 of 768 on average and up to 2235 76 / 77 and 108 / 130.  D = 128: 64 of up to 909 97 / 107 and 162 /
+//            207; 16 of 1024 130 / 117 and 232 / 216; 16 of up to 2235 115 / 104 and 193 / 184.
+//   dQ       (the whole backward) D = 64: 64 of up to 909 175 / 195 and 315 / 358; 16 of 1024 211 / 218 and 369 / 375; 8 of 2048 323 / 309 and
+//            646 / 622.  D = 128: 335 / 359 and 573 / 613; 414 / 418 and 754 / 755; 616 / 594 and 1203 / 1167.
+static bool fwd_in_cols(const PackedDims& d) { return d.max_len < (d.D == 128 ? 960 : d.Hq > d.Hkv ? 2560 : 2048); }
+static bool dq_narrow(const PackedDims& d) { return d.max_len <= 4 * TR; }
+
 size_t muse_packed_fwd_ws_bytes(const PackedDims&) { return 0; }
 size_t muse_packed_bwd_ws_bytes(const PackedDims& d) { return (size_t)d.Hq * d.T * 4; }
 
 int muse_launch_packed_fwd(const PackedDims& d, const void* Q, const void* K, const void* V, const int32_t* cu, void* O, float* LSE, void*, hipStream_t st) {
-  if (d.dtype == MUSE_DTYPE_BF16) return muse_launch_packed_fwd_mfma(d, Q, K, V, cu, O, LSE, st);
-  return muse_launch_packed_fwd_f32(d, (const float*)Q, (const float*)K, (const float*)V, cu, (float*)O, LSE, st);
+  if (d.dtype == MUSE_DTYPE_FP32) return muse_launch_packed_fwd_f32(d, (const float*)Q, (const float*)K, (const float*)V, cu, (float*)O, LSE, st);
+  return fwd_in_cols(d) ? muse_launch_packed_fwd_cols(d, Q, K, V, cu, O, LSE, st) : muse_launch_packed_fwd_mfma(d, Q, K, V, cu, O, LSE, st);
 }
 
 int muse_launch_packed_bwd(const PackedDims& d, const void* Q, const void* K, const void* V, const int32_t* cu, const void* O, const float* LSE,
@@ -120,7 +130,7 @@ int muse_launch_packed_bwd(const PackedDims& d, const void* Q, const void* K, co
     MUSE_LAUNCH_CHECK();
   }
   MuseProf prof_("k_packed_dq", st);
-  if (d.max_len < 4 * TR) return muse_launch_packed_dq_narrow(d, Q, K, V, cu, dO, LSE, delta, dQ, st);
+  if (dq_narrow(d)) return muse_launch_packed_dq_narrow(d, Q, K, V, cu, dO, LSE, delta, dQ, st);
   auto go = [&](auto* kernel, auto* out) {
     const PackedBwd l = lay(TR, d.dq, d.dq);
     hipLaunchKernelGGL(kernel, dim3((unsigned)packed_grid(d.Hq, l.slots)), dim3(256), 0, st, (const bf16_t*)Q, (const bf16_t*)K, (const bf16_t*)V,
