@@ -21,9 +21,10 @@ struct Cols {
     l = 0.f;
   }
   // 64 keys.  kf(h, x): the operand of keys 32 h .. and dims 16 x ..; vf(g, t): that of keys 16 g .. and dims 32 t ..; zs(g) > 0: what scores
-  // of the keys 16 g .. are multiplied by (log2 units), vs(g) what their weights are; hide: keys behind `last` (counted in the tile) are not seen.
+  // of the keys 16 g .. are multiplied by (log2 units), vs(g) what their weights are; hide: keys behind `last` (counted in the tile) are not seen;
+  // dead: bit g, nobody sees the keys 16 g ...
   template <typename KF, typename VF, typename ZS, typename VS>
-  __device__ __forceinline__ void attend(KF kf, VF vf, ZS zs, VS vs, bool hide, int last, int half) {
+  __device__ __forceinline__ void attend(KF kf, VF vf, ZS zs, VS vs, bool hide, int last, int half, uint32_t dead = 0) {
     f32x16_t s[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -36,6 +37,12 @@ struct Cols {
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[h][e] = 32 * h + 8 * (e / 4) + e % 4 <= last - 4 * half ? s[h][e] : MUSE_NEG_INF;
+    }
+    if (dead) {
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[g / 2][8 * (g % 2) + e] = dead >> g & 1 ? MUSE_NEG_INF : s[g / 2][8 * (g % 2) + e];
     }
     float top = MUSE_NEG_INF;
 #pragma unroll
