@@ -64,15 +64,17 @@ struct F32Place {
   size_t qh, kh;             // the head's first row: dense in the tensors, packed in LSE
   bool ok;
 };
+template <int PER>
 __device__ __forceinline__ F32Place place_of(const DenseF32& l, bool keys) {
   const TileId id = tile_id((l.N + 63) / 64, !keys);
   const int G = l.Hq / l.Hkv, H = keys ? l.Hkv : l.Hq, h = id.row % H, b = id.row / H, hk = keys ? h : h / G;
   return {id.tile * 64, 0, l.N, keys ? h * G : h, hk, ((size_t)b * l.Hq + (keys ? h * G : h)) * l.N, ((size_t)b * l.Hkv + hk) * l.N, true};
 }
+template <int PER>
 __device__ __forceinline__ F32Place place_of(const PackedF32& l, bool keys) {
-  const SeqTile s = packed_tile(l.cu, l.S, l.T, 64, keys ? l.Hkv : l.Hq, l.slots, !keys);
+  const SeqTile s = packed_tile(l.cu, l.S, l.T, PER, keys ? l.Hkv : l.Hq, l.slots, !keys);
   const int G = l.Hq / l.Hkv, hq = keys ? s.h * G : s.h;
-  return {s.beg + s.t * 64, s.beg, s.end, hq, hq / G, (size_t)hq * l.T, 0, s.ok};
+  return {s.beg + s.t * PER, s.beg, s.end, hq, hq / G, (size_t)hq * l.T, 0, s.ok};
 }
 // the first row of a row's block, and the first one behind it
 __device__ __forceinline__ int block_beg(const DenseF32& l, const F32Place&, int n) { return (n / l.Bs) * l.Bs; }
@@ -88,6 +90,30 @@ template <int D>
 __device__ __forceinline__ size_t step_of(const DenseF32&, int) { return D; }
 template <int D>
 __device__ __forceinline__ size_t step_of(const PackedF32& l, int i) { return l.r[i].token; }
+// Few tiles (packed, SPLIT): the waves of a workgroup share 16 (D = 128: 32) rows, and each has the same 16 of every 64 (32) staged rows;
+// their sums are added up at the end, in the order of the waves.
+template <int D>
+constexpr int kSplit = F32Attn<D>::kSub;  // waves of a row tile
+
+// this wave's sums go to LDS ...
+template <int D>
+__device__ __forceinline__ void leave_sums(const f32x4_t (&acc)[D / 16], float* a, float* b, int w) {
+  float* to = D == 64 ? a + w * 1024 : (w < 2 ? a : b) + w % 2 * 2048;
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4_t*>(to + i * 256 + threadIdx.x % 64 * 4) = acc[i];
+}
+// ... and the first wave of a row tile adds those of the i-th wave, times mul, to its own
+template <int D>
+__device__ __forceinline__ void add_sums(f32x4_t (&acc)[D / 16], const float* a, const float* b, int w, float mul) {
+  const float* from = D == 64 ? a + w * 1024 : (w < 2 ? a : b) + w % 2 * 2048;
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) {
+    const f32x4_t x = *reinterpret_cast<const f32x4_t*>(from + i * 256 + threadIdx.x % 64 * 4);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) acc[i][t] = fmaf(mul, x[t], acc[i][t]);
+  }
+}
+
 // rows from one head to the next in LSE
 __device__ __forceinline__ size_t lse_rows(const DenseF32& l) { return l.N; }
 __device__ __forceinline__ size_t lse_rows(const PackedF32& l) { return l.T; }
@@ -201,7 +227,7 @@ __device__ __forceinline__ void store_col(const f32x4_t (&acc)[D / 16], float* _
     }
 }
 
-template <int D, typename L>
+template <int D, typename L, int SPLIT = 1>
 __global__ void __launch_bounds__(256, 2) k_attn_fwd_f32(const float* __restrict__ Q, const float* __restrict__ K,
                                                           const float* __restrict__ V, const float* __restrict__ ff,
                                                           float* __restrict__ O, float* __restrict__ LSE, L lay, float scale) {
@@ -209,13 +235,13 @@ __global__ void __launch_bounds__(256, 2) k_attn_fwd_f32(const float* __restrict
   constexpr int R = A::kRows, LD = A::kLd;
   __shared__ __align__(16) float ks[R * LD];
   __shared__ __align__(16) float vs[R * LD];
-  const F32Place at = place_of(lay, false);
+  const F32Place at = place_of<64 / SPLIT>(lay, false);
   if (L::kPacked && !at.ok) return;
   const size_t qh = at.qh, k_step = step_of<D>(lay, 1), v_step = step_of<D>(lay, 2);
   const float *Kh = K + head_of<D>(lay, 1, at.hk, at.kh), *Vh = V + head_of<D>(lay, 2, at.hk, at.kh);
   const int N = at.end, q0 = at.r0, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int c = threadIdx.x % 16, h = (threadIdx.x % 64) / 16;
-  const int qa = q0 + 16 * w, qz = min(qa + 15, N - 1), n = qa + c;  // the wave's first and last query, the lane's
+  const int qa = q0 + 16 * (w / SPLIT), qz = min(qa + 15, N - 1), n = qa + c;  // the wave's first and last query, the lane's
   const bool live = n < N;
   const int beg_a = block_beg(lay, at, qa), beg_z = block_beg(lay, at, qz), beg = block_beg(lay, at, n);
   float q[D / 4];
@@ -224,7 +250,7 @@ __global__ void __launch_bounds__(256, 2) k_attn_fwd_f32(const float* __restrict
 #pragma unroll
   for (int i = 0; i < A::kAcc; ++i) acc[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   float m = MUSE_NEG_INF, l = 0.f;
-  const int kbeg = block_beg(lay, at, q0), kend = min(q0 + 64, N);
+  const int kbeg = block_beg(lay, at, q0), kend = min(q0 + 64 / SPLIT, N);
   float4 kr[4], vr[4];
   fetch_rows<D>(Kh, kbeg, N, kr, k_step);
   fetch_rows<D>(Vh, kbeg, N, vr, v_step);
@@ -235,24 +261,24 @@ __global__ void __launch_bounds__(256, 2) k_attn_fwd_f32(const float* __restrict
     __syncthreads();
     fetch_rows<D>(Kh, k0 + R, N, kr, k_step);
     fetch_rows<D>(Vh, k0 + R, N, vr, v_step);
-    f32x4_t s[A::kSub];
+    f32x4_t s[A::kSub / SPLIT];
     float mx = m;
 #pragma unroll
-    for (int j = 0; j < A::kSub; ++j) {
-      const int kj = k0 + 16 * j;
-      s[j] = f32x4_t{MUSE_NEG_INF, MUSE_NEG_INF, MUSE_NEG_INF, MUSE_NEG_INF};
+    for (int i = 0; i < A::kSub / SPLIT; ++i) {
+      const int j = SPLIT > 1 ? w % SPLIT : i, kj = k0 + 16 * j;
+      s[i] = f32x4_t{MUSE_NEG_INF, MUSE_NEG_INF, MUSE_NEG_INF, MUSE_NEG_INF};
       if (qa < N && kj <= qz && kj + 15 >= beg_a) {
-        s[j] = dot_tile<D>(ks + 16 * j * LD, q, c, h);
+        s[i] = dot_tile<D>(ks + 16 * j * LD, q, c, h);
         if (kj + 15 > qa || kj < beg_z) {
 #pragma unroll
           for (int t = 0; t < 4; ++t) {
             const int key = kj + 4 * h + t;
-            if (key > n || key < beg) s[j][t] = MUSE_NEG_INF;
+            if (key > n || key < beg) s[i][t] = MUSE_NEG_INF;
           }
         }
       }
 #pragma unroll
-      for (int t = 0; t < 4; ++t) mx = fmaxf(mx, s[j][t]);
+      for (int t = 0; t < 4; ++t) mx = fmaxf(mx, s[i][t]);
     }
     mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
@@ -264,20 +290,45 @@ __global__ void __launch_bounds__(256, 2) k_attn_fwd_f32(const float* __restrict
 #pragma unroll
       for (int t = 0; t < 4; ++t) acc[i][t] *= al;
 #pragma unroll
-    for (int j = 0; j < A::kSub; ++j) {
-      const int kj = k0 + 16 * j;
+    for (int i = 0; i < A::kSub / SPLIT; ++i) {
+      const int j = SPLIT > 1 ? w % SPLIT : i, kj = k0 + 16 * j;
       if (qa < N && kj <= qz && kj + 15 >= beg_a) {
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-          s[j][t] = __expf(s[j][t] - ref);
-          l += s[j][t];
+          s[i][t] = __expf(s[i][t] - ref);
+          l += s[i][t];
         }
-        add_tile<D>(acc, vs + 16 * j * LD, s[j], c, h, kj + 15 > qa || kj < beg_z, [&](int r) { return kj + r >= beg && kj + r <= n; });
+        add_tile<D>(acc, vs + 16 * j * LD, s[i], c, h, kj + 15 > qa || kj < beg_z, [&](int r) { return kj + r >= beg && kj + r <= n; });
       }
     }
   }
   l += __shfl_xor(l, 16, 64);
   l += __shfl_xor(l, 32, 64);
+  if constexpr (SPLIT > 1) {
+    __shared__ float ml[4][2][16];
+    __syncthreads();  // the staged rows have been read
+    leave_sums<D>(acc, ks, vs, w);
+    if (h == 0) {
+      ml[w][0][c] = m;
+      ml[w][1][c] = l;
+    }
+    __syncthreads();
+    if (w % SPLIT) return;
+    float top = m;
+    for (int i = 1; i < SPLIT; ++i) top = fmaxf(top, ml[w + i][0][c]);
+    const float ref = top == MUSE_NEG_INF ? 0.f : top, al = __expf(m - ref);
+    l *= al;
+#pragma unroll
+    for (int i = 0; i < A::kAcc; ++i)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) acc[i][t] *= al;
+    for (int i = 1; i < SPLIT; ++i) {
+      const float be = __expf(ml[w + i][0][c] - ref);
+      l = fmaf(be, ml[w + i][1][c], l);
+      add_sums<D>(acc, ks, vs, w + i, be);
+    }
+    m = top;
+  }
   if (!live) return;
   float cf = 0.f;
   const float* f = ff + (qh + n) * D;
@@ -309,7 +360,7 @@ __global__ void __launch_bounds__(256, 2) k_attn_fwd_f32(const float* __restrict
   if (h == 0) LSE[qh + n] = m + __logf(l);
 }
 
-template <int D, typename L>
+template <int D, typename L, int SPLIT = 1>
 __global__ void __launch_bounds__(256, 2) k_attn_bwd_dq_f32(const float* __restrict__ Q, const float* __restrict__ K,
                                                              const float* __restrict__ V, const float* __restrict__ dO,
                                                              const float* __restrict__ LSE, const float* __restrict__ delta,
@@ -318,13 +369,13 @@ __global__ void __launch_bounds__(256, 2) k_attn_bwd_dq_f32(const float* __restr
   constexpr int R = A::kRows, LD = A::kLd;
   __shared__ __align__(16) float ks[R * LD];
   __shared__ __align__(16) float vs[R * LD];
-  const F32Place at = place_of(lay, false);
+  const F32Place at = place_of<64 / SPLIT>(lay, false);
   if (L::kPacked && !at.ok) return;
   const size_t qh = at.qh, k_step = step_of<D>(lay, 1), v_step = step_of<D>(lay, 2);
   const float *Kh = K + head_of<D>(lay, 1, at.hk, at.kh), *Vh = V + head_of<D>(lay, 2, at.hk, at.kh);
   const int N = at.end, q0 = at.r0, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int c = threadIdx.x % 16, h = (threadIdx.x % 64) / 16;
-  const int qa = q0 + 16 * w, qz = min(qa + 15, N - 1), n = qa + c;
+  const int qa = q0 + 16 * (w / SPLIT), qz = min(qa + 15, N - 1), n = qa + c;
   const bool live = n < N;
   const int beg_a = block_beg(lay, at, qa), beg_z = block_beg(lay, at, qz), beg = block_beg(lay, at, n);
   float q[D / 4], g[D / 4];
@@ -334,7 +385,7 @@ __global__ void __launch_bounds__(256, 2) k_attn_bwd_dq_f32(const float* __restr
   f32x4_t acc[A::kAcc];
 #pragma unroll
   for (int i = 0; i < A::kAcc; ++i) acc[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  const int kbeg = block_beg(lay, at, q0), kend = min(q0 + 64, N);
+  const int kbeg = block_beg(lay, at, q0), kend = min(q0 + 64 / SPLIT, N);
   float4 kr[4], vr[4];
   fetch_rows<D>(Kh, kbeg, N, kr, k_step);
   fetch_rows<D>(Vh, kbeg, N, vr, v_step);
@@ -346,8 +397,8 @@ __global__ void __launch_bounds__(256, 2) k_attn_bwd_dq_f32(const float* __restr
     fetch_rows<D>(Kh, k0 + R, N, kr, k_step);
     fetch_rows<D>(Vh, k0 + R, N, vr, v_step);
 #pragma unroll
-    for (int j = 0; j < A::kSub; ++j) {
-      const int kj = k0 + 16 * j;
+    for (int i = 0; i < A::kSub / SPLIT; ++i) {
+      const int j = SPLIT > 1 ? w % SPLIT : i, kj = k0 + 16 * j;
       if (!(qa < N && kj <= qz && kj + 15 >= beg_a)) continue;
       const bool masked = kj + 15 > qa || kj < beg_z;
       const f32x4_t s = dot_tile<D>(ks + 16 * j * LD, q, c, h);
@@ -361,11 +412,18 @@ __global__ void __launch_bounds__(256, 2) k_attn_bwd_dq_f32(const float* __restr
       add_tile<D>(acc, ks + 16 * j * LD, ds, c, h, masked, [&](int r) { return kj + r >= beg && kj + r <= n; });
     }
   }
+  if constexpr (SPLIT > 1) {
+    __syncthreads();
+    leave_sums<D>(acc, ks, vs, w);
+    __syncthreads();
+    if (w % SPLIT) return;
+    for (int i = 1; i < SPLIT; ++i) add_sums<D>(acc, ks, vs, w + i, 1.f);
+  }
   if (live) store_col<D>(acc, dQ + head_of<D>(lay, 5, at.hq, qh) + n * step_of<D>(lay, 5), h, scale);
 }
 
 // loop over the query heads of the group and, inside, the queries n >= m of the key's block
-template <int D, typename L>
+template <int D, typename L, int SPLIT = 1>
 __global__ void __launch_bounds__(256, 2) k_attn_bwd_dkv_f32(const float* __restrict__ Q, const float* __restrict__ K,
                                                               const float* __restrict__ V, const float* __restrict__ dO,
                                                               const float* __restrict__ LSE, const float* __restrict__ delta,
@@ -376,17 +434,17 @@ __global__ void __launch_bounds__(256, 2) k_attn_bwd_dkv_f32(const float* __rest
   __shared__ __align__(16) float gs[R * LD];
   __shared__ __align__(16) float ls[R];
   __shared__ __align__(16) float dls[R];
-  const F32Place at = place_of(lay, true);
+  const F32Place at = place_of<64 / SPLIT>(lay, true);
   if (L::kPacked && !at.ok) return;
   const int N = at.end, G = lay.Hq / lay.Hkv;
   const size_t kh = at.kh, q_step = step_of<D>(lay, 0), g_step = step_of<D>(lay, 4);
   const int k0 = at.r0, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int c = threadIdx.x % 16, h = (threadIdx.x % 64) / 16;
-  const int ka = k0 + 16 * w, kz = min(ka + 15, N - 1), m = ka + c;
+  const int ka = k0 + 16 * (w / SPLIT), kz = min(ka + 15, N - 1), m = ka + c;
   const bool live = m < N;
   // queries end with the block of the key; a tile may straddle blocks
   const int end_a = block_end(lay, at, ka), end_z = min(block_end(lay, at, kz), N), end = min(block_end(lay, at, m), N);
-  const int qend = min(block_end(lay, at, min(k0 + 63, N - 1)), N);
+  const int qend = min(block_end(lay, at, min(k0 + 64 / SPLIT - 1, N - 1)), N);
   float k[D / 4], v[D / 4];
   load_col<D>(K + head_of<D>(lay, 1, at.hk, kh), m, live, h, 1.f, k, step_of<D>(lay, 1));
   load_col<D>(V + head_of<D>(lay, 2, at.hk, kh), m, live, h, 1.f, v, step_of<D>(lay, 2));
@@ -425,8 +483,8 @@ __global__ void __launch_bounds__(256, 2) k_attn_bwd_dkv_f32(const float* __rest
       lr = LSE[qh + min(q0 + R + lrow, N - 1)];
       dr = delta[qh + min(q0 + R + lrow, N - 1)];
 #pragma unroll
-      for (int j = 0; j < A::kSub; ++j) {
-        const int qj = q0 + 16 * j;
+      for (int i = 0; i < A::kSub / SPLIT; ++i) {
+        const int j = SPLIT > 1 ? w % SPLIT : i, qj = q0 + 16 * j;
         if (!(ka < N && qj + 15 >= ka && qj < end_z)) continue;
         const bool masked = qj < kz || qj + 15 >= end_a || qj + 15 >= N;
         f32x4_t p = dot_tile<D>(qs + 16 * j * LD, k, c, h);
@@ -446,6 +504,18 @@ __global__ void __launch_bounds__(256, 2) k_attn_bwd_dkv_f32(const float* __rest
         add_tile<D>(ak, qs + 16 * j * LD, ds, c, h, masked, attends);
       }
     }
+  }
+  if constexpr (SPLIT > 1) {
+    __syncthreads();
+    leave_sums<D>(ak, qs, gs, w);
+    __syncthreads();
+    if (w % SPLIT == 0)
+      for (int i = 1; i < SPLIT; ++i) add_sums<D>(ak, qs, gs, w + i, 1.f);
+    __syncthreads();
+    leave_sums<D>(av, qs, gs, w);
+    __syncthreads();
+    if (w % SPLIT) return;
+    for (int i = 1; i < SPLIT; ++i) add_sums<D>(av, qs, gs, w + i, 1.f);
   }
   if (!live) return;
   store_col<D>(ak, dK + head_of<D>(lay, 6, at.hk, kh) + m * step_of<D>(lay, 6), h, 1.f);
@@ -483,30 +553,43 @@ int muse_launch_attn_bwd_f32(const MuseDims& d, int Bs, const float* Q, const fl
   return MUSE_OK;
 }
 
-static PackedF32 packed_f32(const PackedDims& d, const int32_t* cu) {
-  return {cu, d.S, d.T, d.Hq, d.Hkv, (int)packed_slots(d.T, d.S, 64), {d.q, d.k, d.v, d.o, d.g, d.dq, d.dk, d.dv}};
+static PackedF32 packed_f32(const PackedDims& d, const int32_t* cu, int per) {
+  return {cu, d.S, d.T, d.Hq, d.Hkv, (int)packed_slots(d.T, d.S, per), {d.q, d.k, d.v, d.o, d.g, d.dq, d.dk, d.dv}};
 }
+// The waves of a workgroup share a row tile where tiles of 64 rows would leave the chip idle: the longest tile of a sequence then sets the
+// time.  us, tiles of 64 rows / this, forward and backward: 84 tiles (one sequence of 1400, 4 heads of 2, D = 64) 76 / 35 and 348 /
+// 138, D = 128 136 / 85 and 657 / 381; 248 (4 of 1000) 57 / 47 and 255 / 166, 101 / 97 and 488 / 338; 496 (8 heads) 86 / 69 and 272 / 214,
+// 162 / 139 and 517 / 444; 748 (40 of 300, 4 of 2) 38 / 46 and 136 / 147, 78 / 78 and 269 / 265; 1496 67 / 81 and 209 / 267.
+static bool few_tiles(const PackedDims& d, int heads) { return ((long long)d.T / 64 + 1) * heads < 640; }
 
 int muse_launch_packed_fwd_f32(const PackedDims& d, const float* Q, const float* K, const float* V, const int32_t* cu, float* O, float* LSE, hipStream_t st) {
-  const PackedF32 lay = packed_f32(d, cu);
-  const dim3 g((unsigned)packed_grid(d.Hq, lay.slots));
   MuseProf prof_("k_packed_fwd", st);
-  if (d.D == 64) hipLaunchKernelGGL((k_attn_fwd_f32<64, PackedF32>), g, dim3(256), 0, st, Q, K, V, nullptr, O, LSE, lay, d.scale);
-  else hipLaunchKernelGGL((k_attn_fwd_f32<128, PackedF32>), g, dim3(256), 0, st, Q, K, V, nullptr, O, LSE, lay, d.scale);
+  auto go = [&](auto* kernel, int per) {
+    const PackedF32 lay = packed_f32(d, cu, per);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)packed_grid(d.Hq, lay.slots)), dim3(256), 0, st, Q, K, V, nullptr, O, LSE, lay, d.scale);
+  };
+  if (few_tiles(d, d.Hq)) d.D == 64 ? go(k_attn_fwd_f32<64, PackedF32, kSplit<64>>, 64 / kSplit<64>) : go(k_attn_fwd_f32<128, PackedF32, kSplit<128>>, 64 / kSplit<128>);
+  else d.D == 64 ? go(k_attn_fwd_f32<64, PackedF32>, 64) : go(k_attn_fwd_f32<128, PackedF32>, 64);
   MUSE_LAUNCH_CHECK();
   return MUSE_OK;
 }
 
 int muse_launch_packed_bwd_f32(const PackedDims& d, const float* Q, const float* K, const float* V, const int32_t* cu, const float* dO, const float* LSE,
                                const float* delta, float* dQ, float* dK, float* dV, hipStream_t st) {
-  const PackedF32 lay = packed_f32(d, cu);
-  const dim3 gq((unsigned)packed_grid(d.Hq, lay.slots)), gk((unsigned)packed_grid(d.Hkv, lay.slots));
-  auto go = [&](auto* dq, auto* dkv) {
-    { MuseProf prof_("k_packed_dkv", st); hipLaunchKernelGGL(dkv, gk, dim3(256), 0, st, Q, K, V, dO, LSE, delta, dK, dV, lay, d.scale); }
-    { MuseProf prof_("k_packed_dq", st); hipLaunchKernelGGL(dq, gq, dim3(256), 0, st, Q, K, V, dO, LSE, delta, dQ, lay, d.scale); }
+  auto dkv = [&](auto* kernel, int per) {
+    const PackedF32 lay = packed_f32(d, cu, per);
+    MuseProf prof_("k_packed_dkv", st);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)packed_grid(d.Hkv, lay.slots)), dim3(256), 0, st, Q, K, V, dO, LSE, delta, dK, dV, lay, d.scale);
   };
-  if (d.D == 64) go(k_attn_bwd_dq_f32<64, PackedF32>, k_attn_bwd_dkv_f32<64, PackedF32>);
-  else go(k_attn_bwd_dq_f32<128, PackedF32>, k_attn_bwd_dkv_f32<128, PackedF32>);
+  auto dq = [&](auto* kernel, int per) {
+    const PackedF32 lay = packed_f32(d, cu, per);
+    MuseProf prof_("k_packed_dq", st);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)packed_grid(d.Hq, lay.slots)), dim3(256), 0, st, Q, K, V, dO, LSE, delta, dQ, lay, d.scale);
+  };
+  if (few_tiles(d, d.Hkv)) d.D == 64 ? dkv(k_attn_bwd_dkv_f32<64, PackedF32, kSplit<64>>, 64 / kSplit<64>) : dkv(k_attn_bwd_dkv_f32<128, PackedF32, kSplit<128>>, 64 / kSplit<128>);
+  else d.D == 64 ? dkv(k_attn_bwd_dkv_f32<64, PackedF32>, 64) : dkv(k_attn_bwd_dkv_f32<128, PackedF32>, 64);
+  if (few_tiles(d, d.Hq)) d.D == 64 ? dq(k_attn_bwd_dq_f32<64, PackedF32, kSplit<64>>, 64 / kSplit<64>) : dq(k_attn_bwd_dq_f32<128, PackedF32, kSplit<128>>, 64 / kSplit<128>);
+  else d.D == 64 ? dq(k_attn_bwd_dq_f32<64, PackedF32>, 64) : dq(k_attn_bwd_dq_f32<128, PackedF32>, 64);
   MUSE_LAUNCH_CHECK();
   return MUSE_OK;
 }

@@ -65,6 +65,14 @@ def test_long_sequences(lens, D):
 
 
 @pytest.mark.parametrize("D", [64, 128])
+def test_many_tiles_in_fp32(D):
+    """More tiles than the form for few of them takes."""
+    lens = [700, 650, 0, 720, 690, 1, 640, 660]
+    Q, K, V, dO, cu, cud = make(lens, 16, 16, D, torch.float32)
+    run_and_check(params(lens, Q, K), Q, K, V, dO, cu, cud)
+
+
+@pytest.mark.parametrize("D", [64, 128])
 def test_fp32_gradients_of_bf16_inputs_and_a_scale(D):
     lens = [130, 3, 400]
     Q, K, V, dO, cu, cud = make(lens, 4, 2, D, torch.bfloat16)
