@@ -334,13 +334,25 @@ class CacheParams:
     torch_dtype = Params.torch_dtype
 
 
-@dataclass
+@dataclass(frozen=True)
 class KVCache:
-    """k [pages, Hkv, page, D] and v [pages, Hkv, D, page] of e4m3 bytes (uint8), k_scale and v_scale [pages, Hkv] fp32."""
+    """k [pages, Hkv, page, D] and v [pages, Hkv, D, page] of e4m3 bytes (uint8), k_scale and v_scale [pages, Hkv] fp32; checked once, here."""
     k: torch.Tensor
     v: torch.Tensor
     k_scale: torch.Tensor
     v_scale: torch.Tensor
+
+    def __post_init__(self):
+        dev = _on_gpu(self.k)
+        if self.k.dim() != 4:
+            raise MuseError(f"cache.k: expected [pages, Hkv, page, D], got {list(self.k.shape)}")
+        pages, Hkv, page, D = self.k.shape
+        put = lambda n, v: object.__setattr__(self, n, v)  # noqa: E731
+        put("_ptrs", (_whole(self.k, "cache.k", (pages, Hkv, page, D), torch.uint8, dev),
+                      _whole(self.v, "cache.v", (pages, Hkv, D, page), torch.uint8, dev),
+                      _whole(self.k_scale, "cache.k_scale", (pages, Hkv), torch.float32, dev),
+                      _whole(self.v_scale, "cache.v_scale", (pages, Hkv), torch.float32, dev)))
+        put("_fits", (pages, Hkv, page, D, dev))
 
 
 def kv_cache(p: CacheParams, device="cuda") -> KVCache:
@@ -449,11 +461,10 @@ def exact_attn_packed_bwd(p: PackedParams, Q, K, V, cu_seqlens, O, LSE, dO, ws=N
 
 
 def _cache_ptrs(p: CacheParams, cu_new, kv_lens, table, cache: KVCache, dev):
-    byte, f32 = torch.uint8, torch.float32
+    if cache._fits != (p.pages, p.Hkv, p.page, p.D, dev):
+        raise MuseError(f"cache: expected {p.pages} pages of {p.Hkv} heads, {p.page} tokens, {p.D} dims on {dev}, got {cache._fits}")
     return ((_whole(cu_new, "cu_new", (p.S + 1,), torch.int32, dev) if cu_new is not None else 0,
-             _whole(kv_lens, "kv_lens", (p.S,), torch.int32, dev), _whole(table, "table", (p.S, p.table_cols), torch.int32, dev)),
-            (_whole(cache.k, "cache.k", (p.pages, p.Hkv, p.page, p.D), byte, dev), _whole(cache.v, "cache.v", (p.pages, p.Hkv, p.D, p.page), byte, dev),
-             _whole(cache.k_scale, "cache.k_scale", (p.pages, p.Hkv), f32, dev), _whole(cache.v_scale, "cache.v_scale", (p.pages, p.Hkv), f32, dev)))
+             _whole(kv_lens, "kv_lens", (p.S,), torch.int32, dev), _whole(table, "table", (p.S, p.table_cols), torch.int32, dev)), cache._ptrs)
 
 
 def exact_attn_cache_append(p: CacheParams, K, V, cu_new, kv_lens, table, cache: KVCache):
