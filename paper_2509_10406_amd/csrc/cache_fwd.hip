@@ -35,6 +35,7 @@ struct CacheWork {  // of one launch
   int W, R, rows;   // workgroups per (head, row tile), row tiles, rows of a tile
   int G, sh;        // query heads per key/value head, log2(page)
   int least;        // units of a share, at the least
+  bool whole;       // sequences are not divided: workgroup w has those of the numbers w, w + W, ..
   int used, join;   // rows of a tile that any sequence may have, rows of a workgroup of k_cache_join
   float *po, *pm;   // partial sums [R][Hkv][2 W][rows][D], (maximum, normaliser) [..][rows][2]
 };
@@ -170,8 +171,8 @@ __device__ __forceinline__ void for_segments(const CacheDims& d, const CacheWork
   for (int r = r0;; r += wk.R) {
     const int tile_last = last_token(wk, r);
     const Found f = find_unit(d, wk, cu, lens, r, tile_last, find, w);
-    // More rows than the caller's bound said: whole sequences, one by one, so that nothing is left to be joined.
-    const bool over = r >= wk.R;
+    // More rows than the caller's bound said: whole sequences, one by one, too, so that nothing is left to be joined.
+    const bool over = wk.whole || r >= wk.R;
     int a = share(wk, f.total, w), before = f.before;
     const int b = share(wk, f.total, w + 1);
     int s = over ? w : f.s;
@@ -684,17 +685,21 @@ Plan plan_of(const CacheDims& d) {
   p.w.rows = 16 * p.rt;
   p.w.R = (int)((rows + p.w.rows - 1) / p.w.rows);
   if (p.w.R > 65535) p.w.R = 65535;
-  p.w.least = p.rt == 8 ? 2 : 1;
-  p.w.used = rows < p.w.rows && p.rt == 1 ? (int)rows : p.w.rows;
   // As many workgroups as the chip holds at once, no more: all have the same work, and one that waits for a place doubles the time (64
   // ragged contexts up to 8k, D = 128: 59 us with 512 workgroups, 69 with 768).  Not more than there are units.
-  const long long units = (long long)d.S * (((long long)d.cols * d.page + UNIT - 1) / UNIT), heads = (long long)d.Hkv * p.w.R;
+  const long long each = ((long long)d.cols * d.page + UNIT - 1) / UNIT, heads = (long long)d.Hkv * p.w.R;
   const int per_cu = p.rt == 8 ? 2 : p.rt > 1 ? 1 : d.D == 64 && d.dtype == MUSE_DTYPE_BF16 ? 3 : 2;
   long long W = 256 * per_cu / heads;
-  if (W > units) W = units;
+  // Short contexts are not divided where the chip is full without that, or where there are few rows: the second launch would take longer than
+  // a workgroup does (one context of 1000, 8 heads: 9.2 us for 6.4 + 4.7).
+  p.w.whole = each <= 4 && (p.rt == 1 || d.S * heads >= 256 * per_cu);
+  const long long most = p.w.whole ? d.S : d.S * each;
+  if (W > most) W = most;
   p.w.W = (int)(W < 1 ? 1 : W);
+  p.w.least = p.rt == 8 ? 2 : 1;  // a part of 128 rows costs as much as half a unit (8 pieces of up to 300: 56 + 15.7 us; 1: 56 + 17, 3: 64 + 14)
+  p.w.used = rows < p.w.rows && p.rt == 1 ? (int)rows : p.w.rows;
   p.w.join = p.rt > 1 ? 32 : p.w.W > 8 * d.S ? 1 : 4;
-  if (p.w.W > 1) {
+  if (p.w.W > 1 && !p.w.whole) {
     const size_t slots = (size_t)heads * 2 * p.w.W * p.w.rows;
     p.po = slots * d.D * 4;
     p.bytes = p.po + slots * 8;
@@ -718,7 +723,7 @@ int muse_launch_cache_fwd(const CacheDims& d, const void* Q, const int32_t* cu, 
       hipLaunchKernelGGL(kernel, dim3(p.w.W, d.Hkv, p.w.R), dim3(256), 0, st, d, p.w, (const E*)Q, cu, lens, table, (const uint8_t*)kc, (const uint8_t*)vc, ks,
                          vs, (E*)O, LSE);
     }
-    if (p.w.W > 1) {
+    if (p.bytes) {
       MuseProf prof_("k_cache_join", st);
       hipLaunchKernelGGL(join, dim3(d.S < p.w.W ? d.S : p.w.W - 1, d.Hkv * ((p.w.used + p.w.join - 1) / p.w.join), p.w.R), dim3(256), 0, st, d, p.w, cu, lens, (E*)O, LSE);
     }

@@ -92,6 +92,17 @@ def test_head_layouts(name, Hq, Hkv, dtype):
     b.check_attend()
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("pairs", [[(3000, 4), (40, 4), (1800, 3)], [(2900, 9), (1, 1), (1300, 8)], [(3000, 200), (5000, 90), (7, 7)],
+                                   [(2000 + 10 * i, 2) for i in range(70)]])
+def test_divided_contexts(pairs, D, dtype):
+    """Contexts of several workgroups, in every tile of rows; more sequences than lanes."""
+    b = Batch(pairs, 8, 2, D, 64, dtype)
+    b.check_append()
+    b.check_attend()
+
+
 @pytest.mark.parametrize("page", [16, 128])
 def test_prompt_in_one_piece_is_packed_attention_of_what_is_stored(page):
     """A prompt whose keys and values are e4m3 values: stored and attended it gives what exact_attn_packed_fwd gives, within both bounds."""
