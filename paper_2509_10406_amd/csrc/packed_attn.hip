@@ -8,6 +8,8 @@ int muse_launch_packed_fwd_cols(const PackedDims& d, const void* Q, const void* 
 int muse_launch_packed_fwd_f32(const PackedDims& d, const float* Q, const float* K, const float* V, const int32_t* cu, float* O, float* LSE, hipStream_t st);
 int muse_launch_packed_bwd_f32(const PackedDims& d, const float* Q, const float* K, const float* V, const int32_t* cu, const float* dO, const float* LSE,
                                const float* delta, float* dQ, float* dK, float* dV, hipStream_t st);
+int muse_launch_packed_dkv_cols(const PackedDims& d, const void* Q, const void* K, const void* V, const int32_t* cu, const void* dO, const float* LSE,
+                                const float* delta, void* dK, void* dV, hipStream_t st);
 int muse_launch_packed_dq_narrow(const PackedDims& d, const void* Q, const void* K, const void* V, const int32_t* cu, const void* dO, const float* LSE,
                                  const float* delta, void* dQ, hipStream_t st);
 
@@ -82,8 +84,12 @@ __global__ void __launch_bounds__(256) k_packed_delta(PackedDims d, int slots, c
 //            207; 16 of 1024 130 / 117 and 232 / 216; 16 of up to 2235 115 / 104 and 193 / 184.
 //   dQ       (the whole backward) D = 64: 64 of up to 909 175 / 195 and 315 / 358; 16 of 1024 211 / 218 and 369 / 375; 8 of 2048 323 / 309 and
 //            646 / 622.  D = 128: 335 / 359 and 573 / 613; 414 / 418 and 754 / 755; 616 / 594 and 1203 / 1167.
+//   dK, dV   (the whole backward) D = 64, tiles of 128 / of 256 keys: 400 of 20 133 / 204 and 204 / 266; 200 of 60 106 / 140 and 154 / 182; 128 of
+//            128 168 / 163 and 202 / 202; 64 of 256 125 / 131 and 179 / 170; 40 of 400 157 / 166 and 289 / 268; 25 of 640 153 / 156 and
+//            273 / 264; 16 of 1024 209 / 208.
 static bool fwd_in_cols(const PackedDims& d) { return d.max_len < (d.D == 128 ? 960 : d.Hq > d.Hkv ? 2560 : 2048); }
 static bool dq_narrow(const PackedDims& d) { return d.max_len <= 4 * TR; }
+static bool dkv_in_cols(const PackedDims& d) { return d.D == 64 && d.max_len <= (d.Hq > d.Hkv ? 192 : 640); }
 
 size_t muse_packed_fwd_ws_bytes(const PackedDims&) { return 0; }
 size_t muse_packed_bwd_ws_bytes(const PackedDims& d) { return (size_t)d.Hq * d.T * 4; }
@@ -114,7 +120,10 @@ int muse_launch_packed_bwd(const PackedDims& d, const void* Q, const void* K, co
   auto lay = [&](int tr, const Rows& a, const Rows& b) {
     return PackedBwd{cu, d.S, d.T, d.Hq, d.Hkv, (int)packed_slots(d.T, d.S, tr), d.q, d.k, d.v, d.g, a, b};
   };
-  {
+  if (dkv_in_cols(d)) {
+    MuseProf prof_("k_packed_dkv", st);
+    if (const int rc = muse_launch_packed_dkv_cols(d, Q, K, V, cu, dO, LSE, delta, dK, dV, st)) return rc;
+  } else {
     MuseProf prof_("k_packed_dkv", st);
     auto go = [&](auto* kernel, int tr, auto* k, auto* v) {
       const PackedBwd l = lay(tr, d.dk, d.dv);

@@ -64,6 +64,14 @@ def test_long_sequences(lens, D):
     run_and_check(params(lens, Q, K), Q, K, V, dO, cu, cud)
 
 
+@pytest.mark.parametrize("grad", [mb.BF16, mb.FP32])
+@pytest.mark.parametrize("Hq,Hkv,lens", [(3, 3, [640, 0, 513, 129, 1]), (12, 4, [192, 1, 127, 0, 65, 129])])
+def test_short_sequences(Hq, Hkv, lens, grad):
+    """The kernels of 128 rows, with and without grouped heads."""
+    Q, K, V, dO, cu, cud = make(lens, Hq, Hkv, 64, torch.bfloat16)
+    run_and_check(params(lens, Q, K, grad=grad), Q, K, V, dO, cu, cud)
+
+
 @pytest.mark.parametrize("D", [64, 128])
 def test_many_tiles_in_fp32(D):
     """More tiles than the form for few of them takes."""
