@@ -334,7 +334,7 @@ class CacheParams:
     torch_dtype = Params.torch_dtype
 
 
-@dataclass(frozen=True)
+@dataclass(frozen=True, eq=False)
 class KVCache:
     """k [pages, Hkv, page, D] and v [pages, Hkv, D, page] of e4m3 bytes (uint8), k_scale and v_scale [pages, Hkv] fp32; checked once, here."""
     k: torch.Tensor

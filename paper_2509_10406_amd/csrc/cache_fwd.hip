@@ -36,7 +36,7 @@ struct CacheWork {  // of one launch
   int G, sh;        // query heads per key/value head, log2(page)
   int least;        // units of a share, at the least
   bool whole;       // sequences are not divided: workgroup w has those of the numbers w, w + W, ..
-  int used, join;   // rows of a tile that any sequence may have, rows of a workgroup of k_cache_join
+  int used, join;   // rows of a tile that sequences have by the caller's bound, rows of a workgroup of the joining kernel
   float *po, *pm;   // partial sums [R][Hkv][2 W][rows][D], (maximum, normaliser) [..][rows][2]
 };
 
@@ -62,14 +62,15 @@ __device__ __forceinline__ Seg seg_of(const CacheDims& d, const CacheWork& w, co
 // the new token that the last row of a tile is of
 __device__ __forceinline__ int last_token(const CacheWork& w, int r) { return ((r + 1) * w.rows - 1) / w.G; }
 
-// All units of a row tile in a row: their number, the most new tokens of a sequence; and either where the first unit of workgroup x's
+// All units of a row tile in a row: their number; whether a sequence has rows in the tile w.R further on; and either where the first unit of workgroup x's
 // share lies (its sequence, the units in front of that), or the units in front of sequence x.  Up to 64 sequences: every wave by
 // itself, a lane each; else the 256 threads together, each with a run of the sequences.
 struct Found {
-  int total, before, s, most;
+  int total, before, s;
+  bool more;
 };
 struct FindLds {
-  int sum[4], most[4], before, s;
+  int sum[4], before, s, more;
 };
 // The first unit of workgroup w's share, and whose share a unit is in.  A share has `least` units, so the last workgroups may have none.
 __device__ __forceinline__ int shares(const CacheWork& w, int total) { return min(w.W, max(total / w.least, 1)); }
@@ -87,35 +88,34 @@ __device__ __forceinline__ Found find_unit(const CacheDims& d, const CacheWork& 
     const int upto = scan64(g.units);
     Found f;
     f.total = __builtin_amdgcn_readlane(upto, 63);
-    f.most = __builtin_amdgcn_readfirstlane((int)wave_max((float)g.n));  // a bound is enough: n or the float above it
+    f.more = __builtin_amdgcn_ballot_w64(g.n * w.G > (r + w.R) * w.rows) != 0;
     const int a = share(w, f.total, x);
     f.s = by_seq ? x : a < f.total ? __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > a)) : 0;
     f.before = f.s ? __builtin_amdgcn_readlane(upto, f.s - 1) : 0;
     return f;
   }
   const int tid = threadIdx.x, lane = tid % 64, per = (d.S + 255) / 256, s0 = tid * per, s1 = min(s0 + per, d.S);
-  int mine = 0, most = 0;
+  int mine = 0;
+  bool more = false;
   for (int s = s0; s < s1; ++s) {
     const Seg g = seg_of(d, w, cu, lens, s, r, tile_last);
     mine += g.units;
-    most = max(most, g.n);
+    more = more || g.n * w.G > (r + w.R) * w.rows;
   }
   int upto = mine;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
     const int v = __shfl_up(upto, o, 64);
     if (lane >= o) upto += v;
-    most = max(most, __shfl_xor(most, o, 64));
   }
   __syncthreads();  // what an earlier call left has been read
   if (lane == 63) lds.sum[tid / 64] = upto;
-  if (lane == 0) lds.most[tid / 64] = most;
-  if (tid == 0) lds.s = lds.before = 0;  // of a share that begins behind the last unit: no place, but an index
+  if (tid == 0) lds.s = lds.before = lds.more = 0;  // of a share that begins behind the last unit: no place, but an index
   __syncthreads();
   Found f;
   f.total = __builtin_amdgcn_readfirstlane(lds.sum[0] + lds.sum[1] + lds.sum[2] + lds.sum[3]);
-  f.most = __builtin_amdgcn_readfirstlane(max(max(lds.most[0], lds.most[1]), max(lds.most[2], lds.most[3])));
   for (int i = 0; i < tid / 64; ++i) upto += lds.sum[i];
+  if (more) lds.more = 1;
   const int a = share(w, f.total, x);
   if (by_seq ? s0 <= x && x < s1 : upto - mine <= a && a < upto) {
     int b = upto - mine;
@@ -132,6 +132,7 @@ __device__ __forceinline__ Found find_unit(const CacheDims& d, const CacheWork& 
   __syncthreads();
   f.s = __builtin_amdgcn_readfirstlane(lds.s);
   f.before = __builtin_amdgcn_readfirstlane(lds.before);
+  f.more = __builtin_amdgcn_readfirstlane(lds.more) != 0;
   return f;
 }
 
@@ -188,7 +189,7 @@ __device__ __forceinline__ void for_segments(const CacheDims& d, const CacheWork
         ++s;
       }
     }
-    if ((r + wk.R) * wk.rows >= f.most * wk.G) break;
+    if (!f.more) break;
   }
 }
 
@@ -566,8 +567,10 @@ __global__ void __launch_bounds__(256) k_cache_join(CacheDims d, CacheWork wk, c
   if (p.n < 2) return;
   const int n = p.n;
   const bool together = wk.join == 1 && n > FEW;
-  const int rows = min(first + wk.join, p.sg.n * wk.G - r * wk.rows);
-  for (int q = first + (together ? 0 : wave); q < rows; q += together ? 1 : 4) {
+  if (!together && wave >= wk.join) return;
+  const int rows = min(16, p.sg.n * wk.G - r * 16);
+  // join is 1 or 4; rows beyond the caller's bound (`used`) go round once more
+  for (int q = first + (together ? 0 : wave % wk.join); q < rows; q += groups * wk.join) {
     const int i0 = together ? n * wave / 4 : 0, i1 = together ? n * (wave + 1) / 4 : n;
     float M = MUSE_NEG_INF;
     for (int i = lane; i < n; i += 64) M = fmaxf(M, wk.pm[(p.at(i, 16) + q) * 2]);

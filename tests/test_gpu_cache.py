@@ -216,9 +216,10 @@ def test_shared_pages():
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
-@pytest.mark.parametrize("max_new", [0, 1, 5000])
-def test_the_bound_on_new_tokens_is_a_hint(max_new, dtype):
-    b = Batch([(300, 70), (90, 1), (33, 33)], 8, 2, 64, 32, dtype)
+@pytest.mark.parametrize("max_new", [0, 1, 7, 5000])
+@pytest.mark.parametrize("pairs", [[(300, 70), (90, 1), (33, 33)], [(3000, 70), (90, 1), (1500, 150)], [(20 + i, 1 + i % 40) for i in range(40, 110)]])
+def test_the_bound_on_new_tokens_is_a_hint(pairs, max_new, dtype):
+    b = Batch(pairs, 8, 2, 64, 32, dtype)
     b.p = mb.CacheParams(**{**{f: getattr(b.p, f) for f in b.p.__dataclass_fields__}, "max_new": max_new})
     b.check_append()
     b.check_attend()

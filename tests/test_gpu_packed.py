@@ -103,6 +103,16 @@ def test_the_bound_on_lengths_is_a_hint(max_len, dtype):
     run_and_check(params(lens, Q, K, max_len=max_len), Q, K, V, dO, cu, cud)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Hq,Hkv", HEADS)
+@pytest.mark.parametrize("name", list(LENS))
+def test_without_a_bound(name, Hq, Hkv, D):
+    """No bound on the lengths: the kernels of long sequences, whatever the lengths are."""
+    lens = LENS[name] + [0, 0]
+    Q, K, V, dO, cu, cud = make(lens, Hq, Hkv, D, torch.bfloat16, behind=2700)   # with their rows, T is past every line
+    run_and_check(params(lens, Q, K, max_len=0), Q, K, V, dO, cu, cud, name)
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("D", [64, 128])
 def test_rows_of_no_sequence_are_left(D, dtype):
