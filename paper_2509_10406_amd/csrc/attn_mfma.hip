@@ -771,7 +771,7 @@ int muse_launch_attn_bwd_mfma(const MuseDims& d, int Bs, const void* Q, const vo
   return MUSE_OK;
 }
 
-// dQ of packed sequences whose lengths are short (attn_bwd.hip says where the line is)
+// dQ of packed sequences whose lengths are short (packed_attn.hip says where the line is)
 int muse_launch_packed_dq_narrow(const PackedDims& d, const void* Q, const void* K, const void* V, const int32_t* cu, const void* dO, const float* LSE,
                                  const float* delta, void* dQ, hipStream_t st) {
   const int slots = (int)packed_slots(d.T, d.S, 128);

@@ -17,6 +17,7 @@
 // the workgroups of a (head, row tile): a long context is shared by many, a workgroup may have several short ones.  A
 // sequence that lies inside one workgroup's share is finished there; of the others every workgroup leaves (sum, maximum,
 // normaliser) and a second kernel joins them, in the order of the keys: results do not depend on timing.
+// 32 heads of 8, D = 128: two contexts of 131072 99 us, 537 MB at 5.4 TB/s; 64 ragged ones of up to 8k 59 us, 304 MB at 5.2.
 #include <type_traits>
 
 #include "attn_cols.h"
@@ -411,6 +412,7 @@ __global__ void __launch_bounds__(256, RT > 1 ? 1 : D == 64 && sizeof(T) == 2 ? 
 // values as bf16 in LDS, converted once for all rows (k_cache_fwd would convert them again for every 16 to 64).  Keys lie row by row (lds_tile.h);
 // values as they come, dims first, a dim's 16 keys in the order of the weights' operand (accumulator rows 4 h .. and 8 + 4 h .. of half
 // h side by side), the 16-byte chunks of a dim's 64 keys changed places by bits of the dim so that 16 dims reach all banks.
+// 8 pieces of up to 289 tokens on contexts of up to 3.5k, 16 heads of 4, D = 128: 55 us, bound by conversions and vector work.
 template <int D>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) k_cache_fwd_cols(
     CacheDims d, CacheWork wk, const bf16_t* __restrict__ Q, const int32_t* __restrict__ cu, const int32_t* __restrict__ lens,
@@ -554,7 +556,7 @@ __device__ __forceinline__ Parts parts_of(const CacheDims& d, const CacheWork& w
 }
 
 // Few rows (tiles of 16): bound by the latency of its reads.  A workgroup has one row, and its waves a quarter of the parts each where there
-// are many (joined in order, through LDS), or a row per wave.
+// are many (joined in order, through LDS), or a row per wave.  5.4 us for two contexts of 131072, 6.1 for 64 ragged ones, 32 heads, D = 128.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) k_cache_join(CacheDims d, CacheWork wk, const int32_t* __restrict__ cu, const int32_t* __restrict__ lens,
                                                     T* __restrict__ O, float* __restrict__ LSE) {
@@ -625,6 +627,7 @@ __global__ void __launch_bounds__(256) k_cache_join(CacheDims d, CacheWork wk, c
 }
 
 // Many rows (tiles of 32, 64 or 128, bf16): a workgroup has 32 rows, a thread four dims of D / 32 of them, whose parts it asks for together.
+// 15.6 us for 1571 rows of 16 heads, D = 128, in 8 sequences.
 template <int D>
 __global__ void __launch_bounds__(256) k_cache_join_rows(CacheDims d, CacheWork wk, const int32_t* __restrict__ cu, const int32_t* __restrict__ lens,
                                                          bf16_t* __restrict__ O, float* __restrict__ LSE) {

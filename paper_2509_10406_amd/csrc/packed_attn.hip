@@ -19,9 +19,10 @@ constexpr int FEW = 64;  // rows of a tile of delta, and keys that count as few
 
 // delta_i = dO_i . O_i = sum_j P_ij dP_ij.  O has been rounded to bf16: dS = P (dP - delta) then is off by 2^-8 of dO . O, which does not
 // matter where dP - delta is as large as dP.  For the first rows of a sequence it is not: with one key it is 0, with few keys the weights
-// are large and so is their share in dK, dQ (sequences of 20 tokens: the gradients' error against 64 bits is 1.6 times
-// that of their own rounding).  So the first 64 rows of every sequence have the second sum, from scores made again: one tile.
-// A workgroup has 64 rows of a head; bound by the reads of O and dO.
+// are large and so is their share in dK, dQ (relative error modelled in 64 bits on the host, random inputs, 20 tokens, D = 64: 2.75e-3,
+// 2.35e-3 by the second sum, 1.67e-3 from the gradients' own rounding alone).  So the first 64 rows of every sequence have the second sum, from scores made again: one tile.
+// A workgroup has 64 rows of a head; bound by the reads of O and dO.  16384 tokens, 32 heads, D = 128: 58 us, 4.6 TB/s; 16000 tokens in 40
+// sequences, 16 heads, D = 64: 18 us, 3.7.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) k_packed_delta(PackedDims d, int slots, const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V,
                                                       const int32_t* __restrict__ cu, const T* __restrict__ O, const float* __restrict__ LSE,

