@@ -234,14 +234,15 @@ int exact_attn_bwd_static(const muse_params* p, const void* Q, const void* K, co
  * cu_seqlens [S+1] int32, device: not decreasing, within 0 .. T; equal neighbours are an empty sequence.  Rows in front of
  * cu_seqlens[0] and from cu_seqlens[S] on belong to no sequence: what the outputs hold there is left as it was.  Values outside 0 .. T
  * are taken as 0 or T; other broken offsets give meaningless results but no access outside the tensors.
- * Any Hq / Hkv; D is 64 or 128; (T / 64 + S + 8) Hq up to 2^23.  A row that is not finite reaches the results of its own sequence only (there, by 0 * inf, also results of
- * up to 255 rows of either side that do not attend to it). */
+ * Any Hq / Hkv; D is 64 or 128; (T / 64 + S + 8) Hq up to 2^23.  A row that is not finite reaches the results of its own
+ * sequence only (there, by 0 * inf, also results of up to 255 rows of either side that do not attend to it). */
 typedef struct { int64_t token, head; } muse_rows;
 typedef struct {
   int32_t S;            /* sequences */
   int32_t Hq, Hkv, D;
   int32_t T;            /* rows (tokens) of the tensors, at most 2^27 */
-  int32_t max_len;      /* a bound on the lengths if the caller has one, 0 if not: it chooses between kernels, results do not depend on it */
+  int32_t max_len;      /* a bound on the lengths if the caller has one, 0 if not: it chooses between kernels, whose results differ
+                           by rounding only; a bound that is too small costs time, nothing else */
   int32_t dtype;        /* MUSE_DTYPE_*: element type of Q, K, V, O, dO */
   int32_t grad_dtype;   /* of dQ, dK, dV: MUSE_DTYPE_FP32 or the same as dtype */
   uint32_t flags;       /* 0 */
@@ -276,7 +277,8 @@ typedef struct {
   int32_t T;            /* rows of the new tokens' tensors */
   int32_t pages, page;  /* page: 16, 32, 64 or 128 tokens */
   int32_t table_cols;
-  int32_t max_new;      /* a bound on the new tokens of a sequence, 0 if there is none: launches are sized by it, results do not depend on it */
+  int32_t max_new;      /* a bound on the new tokens of a sequence, 0 if there is none: launches and tiles are chosen by it, and results
+                           differ by rounding only; a bound that is too small costs time, nothing else */
   int32_t dtype;        /* of Q, O and the new K, V */
   uint32_t flags;       /* 0 */
   float scale;          /* of the logits; 0 -> 1/sqrt(D) */
