@@ -336,7 +336,8 @@ class CacheParams:
 
 @dataclass(frozen=True, eq=False)
 class KVCache:
-    """k [pages, Hkv, page, D] and v [pages, Hkv, D, page] of e4m3 bytes (uint8), k_scale and v_scale [pages, Hkv] fp32; checked once, here."""
+    """k [pages, Hkv, page, D] and v [pages, Hkv, D, page] of e4m3 bytes (uint8), k_scale and v_scale [pages, Hkv] fp32.  A call takes the
+    tensors as they are at that moment: their storage may have been replaced since (a cache that was moved out and back)."""
     k: torch.Tensor
     v: torch.Tensor
     k_scale: torch.Tensor
@@ -346,13 +347,13 @@ class KVCache:
         dev = _on_gpu(self.k)
         if self.k.dim() != 4:
             raise MuseError(f"cache.k: expected [pages, Hkv, page, D], got {list(self.k.shape)}")
-        pages, Hkv, page, D = self.k.shape
-        put = lambda n, v: object.__setattr__(self, n, v)  # noqa: E731
-        put("_ptrs", (_whole(self.k, "cache.k", (pages, Hkv, page, D), torch.uint8, dev),
-                      _whole(self.v, "cache.v", (pages, Hkv, D, page), torch.uint8, dev),
-                      _whole(self.k_scale, "cache.k_scale", (pages, Hkv), torch.float32, dev),
-                      _whole(self.v_scale, "cache.v_scale", (pages, Hkv), torch.float32, dev)))
-        put("_fits", (pages, Hkv, page, D, dev))
+        self._addresses(*self.k.shape, dev)
+
+    def _addresses(self, pages, Hkv, page, D, dev):
+        return (_whole(self.k, "cache.k", (pages, Hkv, page, D), torch.uint8, dev),
+                _whole(self.v, "cache.v", (pages, Hkv, D, page), torch.uint8, dev),
+                _whole(self.k_scale, "cache.k_scale", (pages, Hkv), torch.float32, dev),
+                _whole(self.v_scale, "cache.v_scale", (pages, Hkv), torch.float32, dev))
 
 
 def kv_cache(p: CacheParams, device="cuda") -> KVCache:
@@ -461,10 +462,9 @@ def exact_attn_packed_bwd(p: PackedParams, Q, K, V, cu_seqlens, O, LSE, dO, ws=N
 
 
 def _cache_ptrs(p: CacheParams, cu_new, kv_lens, table, cache: KVCache, dev):
-    if cache._fits != (p.pages, p.Hkv, p.page, p.D, dev):
-        raise MuseError(f"cache: expected {p.pages} pages of {p.Hkv} heads, {p.page} tokens, {p.D} dims on {dev}, got {cache._fits}")
     return ((_whole(cu_new, "cu_new", (p.S + 1,), torch.int32, dev) if cu_new is not None else 0,
-             _whole(kv_lens, "kv_lens", (p.S,), torch.int32, dev), _whole(table, "table", (p.S, p.table_cols), torch.int32, dev)), cache._ptrs)
+             _whole(kv_lens, "kv_lens", (p.S,), torch.int32, dev), _whole(table, "table", (p.S, p.table_cols), torch.int32, dev)),
+            cache._addresses(p.pages, p.Hkv, p.page, p.D, dev))
 
 
 def exact_attn_cache_append(p: CacheParams, K, V, cu_new, kv_lens, table, cache: KVCache):

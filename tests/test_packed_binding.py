@@ -1,0 +1,47 @@
+"""CPU-only: what the binding of packed sequences and of the paged cache hands to the library, on tensors that are taken for device
+tensors; nothing is launched."""
+import pytest
+import torch
+
+from paper_2509_10406_amd import binding as mb
+
+P = dict(S=2, Hq=4, Hkv=2, T=2, D=64, pages=5, page=16, table_cols=3, max_new=1)
+
+
+@pytest.fixture
+def cache(monkeypatch):
+    monkeypatch.setattr(mb, "_on_gpu", lambda t: t.device)
+    return mb.kv_cache(mb.CacheParams(**P), device="cpu")
+
+
+def addresses(cache):
+    p = mb.CacheParams(**P)
+    return mb._cache_ptrs(p, None, torch.zeros(2, dtype=torch.int32), torch.zeros(2, 3, dtype=torch.int32), cache, torch.device("cpu"))[1]
+
+
+@pytest.mark.parametrize("name", ["k", "v", "k_scale", "v_scale"])
+def test_replaced_cache_tensors(cache, name):
+    """A cache that was moved out and back has other addresses; tensors that do not fit any more are refused."""
+    at = ["k", "v", "k_scale", "v_scale"].index(name)
+    t = getattr(cache, name)
+    before = addresses(cache)
+    kept = t.data              # so that the new tensor lies elsewhere
+    t.data = kept.clone()
+    assert t.data_ptr() != kept.data_ptr()
+    after = addresses(cache)
+    assert after[at] == t.data_ptr() and all(a == b for i, (a, b) in enumerate(zip(after, before)) if i != at)
+    for bad in (kept[:1], kept.transpose(0, 1), kept.to(torch.float64), kept[..., None]):
+        t.data = bad
+        with pytest.raises(mb.MuseError, match=f"cache.{name}"):
+            addresses(cache)
+    t.data = kept
+    assert addresses(cache) == before
+
+
+def test_a_cache_that_does_not_fit_the_params(cache):
+    for kw in (dict(pages=6), dict(page=32), dict(Hkv=4), dict(D=128)):
+        p = mb.CacheParams(**(P | kw))
+        with pytest.raises(mb.MuseError, match="cache"):
+            mb._cache_ptrs(p, None, torch.zeros(2, dtype=torch.int32), torch.zeros(2, 3, dtype=torch.int32), cache, torch.device("cpu"))
+    with pytest.raises(mb.MuseError, match="cache.v"):
+        mb.KVCache(cache.k, cache.k, cache.k_scale, cache.v_scale)
