@@ -269,6 +269,7 @@ int exact_attn_packed_bwd(const muse_packed_params* p, const void* Q, const void
  * page table[s][x / page], at place x % page.  Positions are int32, offsets into the cache 64 bits.
  *   table [S, table_cols] int32, device.  Entries that no position below the length needs are not looked at; an entry outside 0 .. pages - 1
  *     is a page without tokens (nothing is stored there, and nothing attends to it), and so are positions from table_cols * page on.
+ *     table_cols * page is at most 2^31 - 1024.
  *   kv_lens [S] int32, device: the length of every sequence, the new tokens of the call included; a negative one counts as 0.
  *   cu_new [S+1] int32, device: rows cu_new[s] .. cu_new[s+1] - 1 of the tensors are sequence s's new tokens (as cu_seqlens above), at
  *     positions kv_lens[s] - n .. kv_lens[s] - 1.  NULL: one new token per sequence, row s (T must be S).  */

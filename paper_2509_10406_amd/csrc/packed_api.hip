@@ -79,8 +79,9 @@ int cache_dims(const muse_cache_params* p, CacheDims* d) {
   if (rc) return rc;
   if (p->pages < 1 || p->table_cols < 1 || p->max_new < 0) return MUSE_ERR_INVALID_ARG;
   if (p->page != 16 && p->page != 32 && p->page != 64 && p->page != 128) return MUSE_ERR_UNSUPPORTED;
-  // positions, rows of a group and units of work are int32
-  if ((long long)p->table_cols * p->page > 0x7fffffffll || (long long)p->T * (p->Hq / p->Hkv) > (1 << 29) ||
+  // Positions, rows of a group and units of work are int32; the attention rounds positions up to a unit of 256 keys and looks at
+  // the table for up to two units further on, which has to stay within 31 bits too.
+  if ((long long)p->table_cols * p->page > 0x80000000ll - 1024 || (long long)p->T * (p->Hq / p->Hkv) > (1 << 29) ||
       (long long)p->S * (((long long)p->table_cols * p->page + 255) / 256 + 1) > 0x7fffffffll)
     return MUSE_ERR_UNSUPPORTED;
   *d = CacheDims{p->S, p->Hq, p->Hkv, p->D, p->T, p->pages, p->page, p->table_cols, p->max_new > 0 && p->max_new < p->T ? p->max_new : p->T,

@@ -1,5 +1,7 @@
 """CPU-only: what the binding of packed sequences and of the paged cache hands to the library, on tensors that are taken for device
-tensors; nothing is launched."""
+tensors, and limits that are checked on the host; nothing is launched."""
+import ctypes as C
+
 import pytest
 import torch
 
@@ -45,3 +47,13 @@ def test_a_cache_that_does_not_fit_the_params(cache):
             mb._cache_ptrs(p, None, torch.zeros(2, dtype=torch.int32), torch.zeros(2, 3, dtype=torch.int32), cache, torch.device("cpu"))
     with pytest.raises(mb.MuseError, match="cache.v"):
         mb.KVCache(cache.k, cache.k, cache.k_scale, cache.v_scale)
+
+
+@pytest.mark.parametrize("page", [16, 128])
+def test_positions_and_the_units_behind_them_are_31_bits(page):
+    """Attention goes by units of 256 keys and asks for the table's entries up to two units ahead: positions end that far below 2^31."""
+    most = (2**31 - 1024) // page
+    for cols, rc in ((most, 0), (most + 1, -2), ((2**31 - 1) // page, -2)):
+        got = C.c_size_t(0)
+        p = mb.CacheParams(**(P | dict(page=page, table_cols=cols)))
+        assert mb.load().muse_cache_workspace_bytes(C.byref(p._c), C.byref(got)) == rc, cols
