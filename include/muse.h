@@ -64,7 +64,7 @@ enum { MUSE_DTYPE_FP32 = 0, MUSE_DTYPE_BF16 = 1 };
  * workspace reuses them instead of recomputing (the usual save-for-backward of a training step).  Needs a
  * workspace that holds all heads at once (the `preferred` size of MUSE_WS_BWD), else
  * MUSE_ERR_WORKSPACE_TOO_SMALL.  muse_fwd stamps the head of the workspace (a hash of the params, the
- * workspace address) after its last kernel; every other entry point that is handed a workspace clears the
+ * workspace address) after its last kernel; every other entry point that writes to a workspace clears the
  * stamp.  muse_bwd reads the stamp back before it launches anything -- this waits for the work queued on
  * `stream` so far, the one place where the library synchronises -- and returns MUSE_ERR_STATE if it does not
  * match.  The stamp cannot see a caller who overwrites the middle of the workspace. */

@@ -565,6 +565,7 @@ __global__ void __launch_bounds__(256) k_cache_join(CacheDims d, CacheWork wk, c
   __shared__ float part[4][D + 1];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64;
   const int groups = (wk.used + wk.join - 1) / wk.join, hk = blockIdx.y / groups, first = blockIdx.y % groups * wk.join, r = blockIdx.z;
+  clear_stamp(wk.po);
   const Parts p = parts_of(d, wk, cu, lens, find, blockIdx.x, hk, r);
   if (p.n < 2) return;
   const int n = p.n;
@@ -634,6 +635,7 @@ __global__ void __launch_bounds__(256) k_cache_join_rows(CacheDims d, CacheWork 
   constexpr int TPR = D / 4, STEP = 256 / TPR, N = 32 / STEP;
   __shared__ FindLds find;
   const int tid = threadIdx.x, groups = wk.rows / 32, hk = blockIdx.y / groups, q0 = blockIdx.y % groups * 32 + tid / TPR, r = blockIdx.z;
+  clear_stamp(wk.po);
   const Parts p = parts_of(d, wk, cu, lens, find, blockIdx.x, hk, r);
   if (p.n < 2) return;
   const int rows = p.sg.n * wk.G - r * wk.rows;
@@ -680,7 +682,7 @@ __global__ void __launch_bounds__(256) k_cache_join_rows(CacheDims d, CacheWork 
 struct Plan {
   CacheWork w;
   int rt;
-  size_t po, bytes;
+  size_t sums, bytes;  // of the partial sums, of the workspace
 };
 Plan plan_of(const CacheDims& d) {
   Plan p{};
@@ -707,8 +709,8 @@ Plan plan_of(const CacheDims& d) {
   p.w.join = p.rt > 1 ? 32 : p.w.W > 8 * d.S ? 1 : 4;
   if (p.w.W > 1 && !p.w.whole) {
     const size_t slots = (size_t)heads * 2 * p.w.W * p.w.rows;
-    p.po = slots * d.D * 4;
-    p.bytes = p.po + slots * 8;
+    p.sums = slots * d.D * 4;
+    p.bytes = kTagBytes + p.sums + slots * 8;
   }
   return p;
 }
@@ -720,8 +722,8 @@ size_t muse_cache_fwd_ws_bytes(const CacheDims& d) { return plan_of(d).bytes; }
 int muse_launch_cache_fwd(const CacheDims& d, const void* Q, const int32_t* cu, const int32_t* lens, const int32_t* table, const void* kc, const void* vc,
                           const float* ks, const float* vs, void* O, float* LSE, void* ws, hipStream_t st) {
   Plan p = plan_of(d);
-  p.w.po = (float*)ws;
-  p.w.pm = (float*)((char*)ws + p.po);
+  p.w.po = (float*)((char*)ws + kTagBytes);
+  p.w.pm = (float*)((char*)ws + kTagBytes + p.sums);
   auto go = [&](auto* kernel, auto* join, auto* t) {
     using E = std::remove_pointer_t<decltype(t)>;
     {

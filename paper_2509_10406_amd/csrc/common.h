@@ -14,6 +14,7 @@ typedef __attribute__((ext_vector_type(16))) float f32x16_t;
 #define MUSE_WAVE 64
 #define MUSE_MAX_CLUSTERS 2048  // largest Cq / Ck the host accepts (LDS tables of the bucketing and chain kernels)
 #define MUSE_NEG_INF (-__builtin_huge_valf())
+constexpr size_t kTagBytes = 256;  // head of every workspace: the stamp of MUSE_FLAG_KEEP_FWD_STATE
 
 __device__ __forceinline__ float bf16_bits_to_f32(bf16_t h) {
   return __uint_as_float(((uint32_t)h) << 16);

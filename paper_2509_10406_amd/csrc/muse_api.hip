@@ -101,8 +101,7 @@ int make_dims(const muse_params* p, bool full, MuseDims* d) {
 }
 
 // ---- stamp at the head of every workspace (MUSE_FLAG_KEEP_FWD_STATE) -------------------------
-// The first kTagBytes of a workspace belong to the stamp; every layout starts behind it.
-constexpr size_t kTagBytes = 256;
+// The first kTagBytes (common.h) of a workspace belong to the stamp; every layout starts behind it.
 constexpr uint64_t kTagMagic = 0x4d755365a7c3f10bull;
 
 __global__ void k_stamp(uint64_t* tag, uint64_t a, uint64_t b, uint64_t c, uint64_t d) {

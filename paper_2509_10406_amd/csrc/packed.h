@@ -110,6 +110,11 @@ __device__ __forceinline__ SeqTile packed_tile(const int32_t* __restrict__ cu, i
   r.ok = r.ok && i < slots;
   return r;
 }
+// A call that writes to a workspace clears the stamp at its head: the first workgroup of a launch does, for a layout that starts at `behind`.
+__device__ __forceinline__ void clear_stamp(float* behind) {
+  if ((blockIdx.x | blockIdx.y | blockIdx.z) == 0 && threadIdx.x < 4) reinterpret_cast<uint64_t*>(behind - kTagBytes / 4)[threadIdx.x] = 0;
+}
+
 static inline long long packed_grid(int H, long long slots) {
   const int turns = H % 8 == 0 ? 1 : H % 4 == 0 ? 2 : H % 2 == 0 ? 4 : 8;
   return (slots + turns - 1) / turns * (H * turns);

@@ -27,6 +27,7 @@ template <typename T, int D>
 __global__ void __launch_bounds__(256) k_packed_delta(PackedDims d, int slots, const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V,
                                                       const int32_t* __restrict__ cu, const T* __restrict__ O, const float* __restrict__ LSE,
                                                       const T* __restrict__ dO, float* __restrict__ delta) {
+  clear_stamp(delta);
   const SeqTile st = packed_tile(cu, d.S, d.T, FEW, d.Hq, slots);
   if (!st.ok) return;
   const int h = st.h, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, r0 = st.beg + st.t * FEW, end = min(r0 + FEW, st.end);
@@ -93,7 +94,7 @@ static bool dq_narrow(const PackedDims& d) { return d.max_len <= 4 * TR; }
 static bool dkv_in_cols(const PackedDims& d) { return d.D == 64 && d.max_len <= (d.Hq > d.Hkv ? 192 : 640); }
 
 size_t muse_packed_fwd_ws_bytes(const PackedDims&) { return 0; }
-size_t muse_packed_bwd_ws_bytes(const PackedDims& d) { return (size_t)d.Hq * d.T * 4; }
+size_t muse_packed_bwd_ws_bytes(const PackedDims& d) { return kTagBytes + (size_t)d.Hq * d.T * 4; }
 
 int muse_launch_packed_fwd(const PackedDims& d, const void* Q, const void* K, const void* V, const int32_t* cu, void* O, float* LSE, void*, hipStream_t st) {
   if (d.dtype == MUSE_DTYPE_FP32) return muse_launch_packed_fwd_f32(d, (const float*)Q, (const float*)K, (const float*)V, cu, (float*)O, LSE, st);
@@ -102,7 +103,7 @@ int muse_launch_packed_fwd(const PackedDims& d, const void* Q, const void* K, co
 
 int muse_launch_packed_bwd(const PackedDims& d, const void* Q, const void* K, const void* V, const int32_t* cu, const void* O, const float* LSE,
                            const void* dO, void* dQ, void* dK, void* dV, void* ws, hipStream_t st) {
-  float* delta = (float*)ws;
+  float* delta = (float*)((char*)ws + kTagBytes);
   {
     const int slots = (int)packed_slots(d.T, d.S, FEW);
     const dim3 g((unsigned)packed_grid(d.Hq, slots));
