@@ -279,7 +279,7 @@ typedef struct {
   int32_t pages, page;  /* page: 16, 32, 64 or 128 tokens */
   int32_t table_cols;
   int32_t max_new;      /* a bound on the new tokens of a sequence, 0 if there is none: launches and tiles are chosen by it, and results
-                           differ by rounding only; a bound that is too small costs time, nothing else */
+                           differ by rounding only; a bound that is too small costs time, nothing else.  Without cu_new it is 1 */
   int32_t dtype;        /* of Q, O and the new K, V */
   uint32_t flags;       /* 0 */
   float scale;          /* of the logits; 0 -> 1/sqrt(D) */

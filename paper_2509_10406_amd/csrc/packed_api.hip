@@ -132,7 +132,10 @@ int exact_attn_cache_append(const muse_cache_params* p, const void* K, const voi
   if (rc) return rc;
   if ((rc = make_rows(p->k, p->T, p->Hkv, p->D, p->dtype, false, &d.k)) || (rc = make_rows(p->v, p->T, p->Hkv, p->D, p->dtype, false, &d.v))) return rc;
   if (!K || !V || !kv_lens || !table || !k_cache || !v_cache || !k_scale || !v_scale || !aligned16({K, V, k_cache, v_cache})) return MUSE_ERR_INVALID_ARG;
-  if (!cu_new && p->T != p->S) return MUSE_ERR_INVALID_ARG;
+  if (!cu_new) {  // one new token per sequence, whatever the caller's bound says
+    if (p->T != p->S) return MUSE_ERR_INVALID_ARG;
+    d.max_new = 1;
+  }
   return muse_launch_cache_append(d, K, V, cu_new, kv_lens, table, k_cache, v_cache, k_scale, v_scale, (hipStream_t)stream);
 }
 
@@ -142,6 +145,11 @@ int muse_cache_workspace_bytes(const muse_cache_params* p, size_t* bytes) {
   const int rc = cache_dims(p, &d);
   if (rc) return rc;
   *bytes = muse_cache_fwd_ws_bytes(d);
+  if (p->T == p->S) {  // a call without cu_new takes the plan of single tokens
+    d.max_new = 1;
+    const size_t single = muse_cache_fwd_ws_bytes(d);
+    if (single > *bytes) *bytes = single;
+  }
   return MUSE_OK;
 }
 
@@ -153,7 +161,10 @@ int exact_attn_cache_fwd(const muse_cache_params* p, const void* Q, const int32_
   if (rc) return rc;
   if ((rc = make_rows(p->q, p->T, p->Hq, p->D, p->dtype, false, &d.q)) || (rc = make_rows(p->o, p->T, p->Hq, p->D, p->dtype, true, &d.o))) return rc;
   if (!Q || !kv_lens || !table || !k_cache || !v_cache || !k_scale || !v_scale || !O || !aligned16({Q, k_cache, v_cache, O})) return MUSE_ERR_INVALID_ARG;
-  if (!cu_new && p->T != p->S) return MUSE_ERR_INVALID_ARG;
+  if (!cu_new) {  // one new token per sequence, whatever the caller's bound says
+    if (p->T != p->S) return MUSE_ERR_INVALID_ARG;
+    d.max_new = 1;
+  }
   const size_t need = muse_cache_fwd_ws_bytes(d);
   if (need && (!ws || (uintptr_t)ws % 256)) return MUSE_ERR_INVALID_ARG;
   if (ws_bytes < need) return MUSE_ERR_WORKSPACE_TOO_SMALL;

@@ -57,3 +57,11 @@ def test_positions_and_the_units_behind_them_are_31_bits(page):
         got = C.c_size_t(0)
         p = mb.CacheParams(**(P | dict(page=page, table_cols=cols)))
         assert mb.load().muse_cache_workspace_bytes(C.byref(p._c), C.byref(got)) == rc, cols
+
+
+@pytest.mark.parametrize("S,dtype", [(64, mb.BF16), (4096, mb.BF16), (4096, mb.FP32), (2, mb.FP32)])
+def test_workspace_of_single_tokens_without_a_bound(S, dtype):
+    """A call without cu_new has one new token per sequence, also where the params hold no bound: the workspace is enough for that plan."""
+    size = lambda n: mb.muse_cache_workspace_bytes(mb.CacheParams(S=S, Hq=32, Hkv=8, T=S, D=128, pages=9, page=64, table_cols=200,  # noqa: E731
+                                                                  max_new=n, dtype=dtype))
+    assert size(0) >= size(1) > 0
