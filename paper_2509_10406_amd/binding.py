@@ -484,7 +484,8 @@ def muse_cache_workspace_bytes(p: CacheParams) -> int:
 
 
 def exact_attn_cache_fwd(p: CacheParams, Q, cu_new, kv_lens, table, cache: KVCache, ws=None, out=None):
-    """Causal attention of the new tokens' queries Q [T, Hq, D] to their sequences' cached tokens.  Returns (O [T, Hq, D], LSE [Hq, T])."""
+    """Causal attention of the new tokens' queries Q [T, Hq, D] to their sequences' cached tokens.  Returns (O [T, Hq, D], LSE [Hq, T]); out:
+    tensors to write them into, its LSE may be None."""
     dev = _on_gpu(Q)
     O, LSE = out if out is not None else (torch.empty(p.T, p.Hq, p.D, dtype=p.torch_dtype, device=dev),
                                           torch.empty(p.Hq, p.T, dtype=torch.float32, device=dev))
@@ -496,7 +497,8 @@ def exact_attn_cache_fwd(p: CacheParams, Q, cu_new, kv_lens, table, cache: KVCac
         need = muse_cache_workspace_bytes(p)
         object.__setattr__(p, "_ws", need)
     keep, at, size = _scratch(need, ws, dev)
-    _packed_call("exact_attn_cache_fwd", dev, pc, qp, *index, *held, op, _whole(LSE, "LSE", (p.Hq, p.T), torch.float32, dev), at, size)
+    _packed_call("exact_attn_cache_fwd", dev, pc, qp, *index, *held, op,
+                 _whole(LSE, "LSE", (p.Hq, p.T), torch.float32, dev) if LSE is not None else 0, at, size)
     return O, LSE
 
 
