@@ -65,3 +65,32 @@ def test_workspace_of_single_tokens_without_a_bound(S, dtype):
     size = lambda n: mb.muse_cache_workspace_bytes(mb.CacheParams(S=S, Hq=32, Hkv=8, T=S, D=128, pages=9, page=64, table_cols=200,  # noqa: E731
                                                                   max_new=n, dtype=dtype))
     assert size(0) >= size(1) > 0
+
+
+def test_tensors_on_another_device_than_the_current_one(monkeypatch):
+    """The call is made on the tensors' device, on that device's current stream."""
+    now, calls = [0], []
+
+    class device:
+        def __init__(self, d):
+            self.to = d.index
+
+        def __enter__(self):
+            self.was, now[0] = now[0], self.to
+
+        def __exit__(self, *_):
+            now[0] = self.was
+
+    class library:
+        @staticmethod
+        def exact_attn_packed_fwd(p, *args):
+            calls.append((now[0], args))
+            return 0
+
+    monkeypatch.setattr(torch.cuda, "device", device)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: now[0], raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda i: 100 + i, raising=False)
+    monkeypatch.setattr(mb, "load", lambda: library)
+    for index in (0, 1):
+        mb._packed_call("exact_attn_packed_fwd", torch.device("cuda", index), mb._PackedParams(), 5)
+    assert calls == [(0, (5, 100)), (1, (5, 101))] and now == [0]
