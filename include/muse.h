@@ -234,7 +234,7 @@ int exact_attn_bwd_static(const muse_params* p, const void* Q, const void* K, co
  * cu_seqlens [S+1] int32, device: not decreasing, within 0 .. T; equal neighbours are an empty sequence.  Rows in front of
  * cu_seqlens[0] and from cu_seqlens[S] on belong to no sequence: what the outputs hold there is left as it was.  Values outside 0 .. T
  * are taken as 0 or T; other broken offsets give meaningless results but no access outside the tensors.
- * Any Hq / Hkv; D is 64 or 128; (T / 64 + S + 8) Hq up to 2^23.  A row that is not finite reaches the results of its own
+ * Any Hq / Hkv; D is 64 or 128; Hq up to 4096, S up to 2^20, (T / 64 + S + 8) Hq up to 2^23 (MUSE_ERR_UNSUPPORTED beyond).  A row that is not finite reaches the results of its own
  * sequence only (there, by 0 * inf, also results of up to 255 rows of either side that do not attend to it). */
 typedef struct { int64_t token, head; } muse_rows;
 typedef struct {
@@ -264,18 +264,18 @@ int exact_attn_packed_bwd(const muse_packed_params* p, const void* Q, const void
 /* ---- A paged cache of 8-bit keys and values ------------------------------------------------------
  * The cache has `pages` pages of `page` tokens.  Per page and key/value head it holds
  *   k_cache [pages, Hkv, page, D], v_cache [pages, Hkv, D, page]  e4m3 (OCP) bytes: a value stands for itself times its scale
- *   k_scale, v_scale [pages, Hkv]  fp32
+ *   k_scale, v_scale [pages, Hkv]  fp32, not negative
  * (values with the dims first, so that the matrix instructions' operand is read as it lies).  The token at position x of sequence s is in
  * page table[s][x / page], at place x % page.  Positions are int32, offsets into the cache 64 bits.
  *   table [S, table_cols] int32, device.  Entries that no position below the length needs are not looked at; an entry outside 0 .. pages - 1
  *     is a page without tokens (nothing is stored there, and nothing attends to it), and so are positions from table_cols * page on.
- *     table_cols * page is at most 2^31 - 1024.
+ *     table_cols * page is at most 2^31 - 1024; S ceil(table_cols * page / 256) + S, what attention counts in, below 2^31.
  *   kv_lens [S] int32, device: the length of every sequence, the new tokens of the call included; a negative one counts as 0.
  *   cu_new [S+1] int32, device: rows cu_new[s] .. cu_new[s+1] - 1 of the tensors are sequence s's new tokens (as cu_seqlens above), at
  *     positions kv_lens[s] - n .. kv_lens[s] - 1.  NULL: one new token per sequence, row s (T must be S).  */
 typedef struct {
   int32_t S, Hq, Hkv, D;
-  int32_t T;            /* rows of the new tokens' tensors */
+  int32_t T;            /* rows of the new tokens' tensors; T Hq / Hkv is at most 2^29.  S and Hq as for packed sequences */
   int32_t pages, page;  /* page: 16, 32, 64 or 128 tokens */
   int32_t table_cols;
   int32_t max_new;      /* a bound on the new tokens of a sequence, 0 if there is none: launches and tiles are chosen by it, and results
@@ -295,7 +295,9 @@ int exact_attn_cache_append(const muse_cache_params* p, const void* K, const voi
                             const int32_t* table, void* k_cache, void* v_cache, float* k_scale, float* v_scale, void* stream);
 
 /* Causal attention of the new tokens' queries to their sequences' cached tokens: the query of position x to the positions 0 .. x.
- * A query without any key (a position below 0, or no page) gets O = 0 and LSE = -inf.  LSE [Hq, T] fp32 (may be NULL). */
+ * A query without any key (a position below 0, or no page) gets O = 0 and LSE = -inf.  LSE [Hq, T] fp32 (may be NULL).
+ * A stored value that is NaN reaches O of its own sequence only; there, by 0 * NaN, also that of queries of the same call at up to
+ * 94 positions in front of it. */
 int muse_cache_workspace_bytes(const muse_cache_params* p, size_t* bytes);
 int exact_attn_cache_fwd(const muse_cache_params* p, const void* Q, const int32_t* cu_new, const int32_t* kv_lens, const int32_t* table,
                          const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,

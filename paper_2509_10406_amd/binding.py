@@ -433,7 +433,8 @@ def _packed_bytes(p: PackedParams, which: int) -> int:
 
 def exact_attn_packed_fwd(p: PackedParams, Q, K, V, cu_seqlens, ws=None, out=None):
     """Exact causal attention of packed sequences.  Q [T, Hq, D], K and V [T, Hkv, D] in any strides whose rows are adjacent elements at
-    16-byte boundaries, cu_seqlens [S + 1] int32.  Returns (O [T, Hq, D], LSE [Hq, T]); out: tensors to write them into."""
+    16-byte boundaries, cu_seqlens [S + 1] int32.  Returns (O [T, Hq, D], LSE [Hq, T]); out: tensors to write them into.  Rows of no sequence
+    keep what out holds there; without out they are not initialised."""
     dev = _on_gpu(Q)
     O, LSE = out if out is not None else (torch.empty(p.T, p.Hq, p.D, dtype=p.torch_dtype, device=dev),
                                           torch.empty(p.Hq, p.T, dtype=torch.float32, device=dev))
@@ -447,7 +448,8 @@ def exact_attn_packed_fwd(p: PackedParams, Q, K, V, cu_seqlens, ws=None, out=Non
 
 
 def exact_attn_packed_bwd(p: PackedParams, Q, K, V, cu_seqlens, O, LSE, dO, ws=None, out=None):
-    """The gradient of exact_attn_packed_fwd.  Returns (dQ, dK, dV) of grad_dtype, shaped as Q, K, V."""
+    """The gradient of exact_attn_packed_fwd.  Returns (dQ, dK, dV) of grad_dtype, shaped as Q, K, V; out: tensors to write them into.  Rows of
+    no sequence (padding) keep what out holds there; without out they are not initialised: a caller that sums over all rows gives zeros."""
     dev = _on_gpu(Q)
     t, gt, pc = p.torch_dtype, p.torch_grad_dtype, _PackedParams.from_buffer_copy(p._c)
     dQ, dK, dV = out if out is not None else (torch.empty(p.T, h, p.D, dtype=gt, device=dev) for h in (p.Hq, p.Hkv, p.Hkv))
@@ -485,7 +487,7 @@ def muse_cache_workspace_bytes(p: CacheParams) -> int:
 
 def exact_attn_cache_fwd(p: CacheParams, Q, cu_new, kv_lens, table, cache: KVCache, ws=None, out=None):
     """Causal attention of the new tokens' queries Q [T, Hq, D] to their sequences' cached tokens.  Returns (O [T, Hq, D], LSE [Hq, T]); out:
-    tensors to write them into, its LSE may be None."""
+    tensors to write them into, its LSE may be None.  Rows of no sequence keep what out holds there; without out they are not initialised."""
     dev = _on_gpu(Q)
     O, LSE = out if out is not None else (torch.empty(p.T, p.Hq, p.D, dtype=p.torch_dtype, device=dev),
                                           torch.empty(p.Hq, p.T, dtype=torch.float32, device=dev))

@@ -24,7 +24,7 @@ bool muse_attn_rows_to_lds(const void* Q, const void* K, const void* V, const vo
   return ((uintptr_t)Q | (uintptr_t)K | (uintptr_t)V | (uintptr_t)dO) % 16 == 0;
 }
 
-// the gradients may leave in bf16 (MuseDims::grads16): all of them come from the kernels of this file
+// the gradients may leave in bf16 (MuseDims::grads16): all of them come from the kernels of attn_bwd_wide.h
 bool muse_attn_bwd_writes16(const MuseDims& d, int Bs, const void* Q, const void* K, const void* V, const void* dO) {
   return d.dtype == MUSE_DTYPE_BF16 && muse_attn_dq_wide(d, Bs) && muse_attn_dkv_wide(d, Bs) && muse_attn_rows_to_lds(Q, K, V, dO);
 }
